@@ -265,6 +265,134 @@ pbb_status_t swa_backward(const pbb_desc_t *desc, int32_t n, const void *q, cons
                           void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
                           void *stream);
 
+/*
+ * Rotary positions of one or several axes.
+ *
+ * Channel pair c < head_dim / 2 (channels c and c + head_dim / 2, the convention of the rotary
+ * decode steps) turns by turns[c] * p whole turns, p the position of the token on axis axis[c]:
+ * text has one axis, images and video have time, height and width.  pbb_rope_init fills the
+ * struct for rates base^(-2c / head_dim) / (2 pi); a caller may change turns[] afterwards (scaled
+ * contexts: any finite rates) and axis[].  The struct is plain data, read on the host at each call.
+ */
+#define PBB_MAX_AXES 4
+typedef struct {
+  int32_t head_dim;  /* 64 or 128 */
+  int32_t n_axes;    /* 1 .. PBB_MAX_AXES */
+  double turns[64];  /* turns per position of each pair; entries from head_dim / 2 on are ignored */
+  uint8_t axis[64];  /* axis of each pair, below n_axes */
+} pbb_rope_t;
+
+/*
+ * Fill *rope on the host.  base > 1.  axis: head_dim / 2 entries below n_axes, or NULL for axis 0
+ * throughout.  PBB_ERR_NULL for a NULL rope, PBB_ERR_SHAPE for the rest; nothing is written then.
+ */
+pbb_status_t pbb_rope_init(pbb_rope_t *rope, int32_t head_dim, double base, int32_t n_axes,
+                           const uint8_t *axis);
+
+/*
+ * Turn n_heads rows of every token by the token's positions: what pbb_prefill, pbb_backward and
+ * their sliding-window counterparts expect of q and k, and (inverse != 0, the transposed rotation)
+ * what takes their gradients dq and dk back to the gradients of the unrotated rows.
+ *   x, out     [n_tokens][n_heads][head_dim], tokens x_stride and out_stride ELEMENTS apart (at
+ *              least n_heads * head_dim; multiples of 16 bytes), rows of a token contiguous: a part
+ *              of a fused projection buffer may be read or written in place
+ *   positions  int32 [n_axes][n_tokens], any value (negative ones turn backwards)
+ * Angles are reduced to a turn in fp64.  float32: fp32 sines and cosines of the reduced angle;
+ * bfloat16: fp32 arithmetic, rounded RNE once.  out may be x itself (with the same stride); other
+ * overlaps are undefined.  0 <= n_tokens <= 2^30 (0 does nothing), 1 <= n_heads,
+ * n_heads * head_dim <= 2^24 (PBB_ERR_SHAPE otherwise).  x, out 16-byte aligned, positions 4-byte.
+ */
+pbb_status_t pbb_rotate(const pbb_rope_t *rope, int32_t n_tokens, int32_t n_heads,
+                        const int32_t *positions, const void *x, int64_t x_stride, void *out,
+                        int64_t out_stride, int32_t inverse, int32_t dtype, void *stream);
+
+/*
+ * Paged KV cache: what the global layers between local ones attend over, and what chunks of a
+ * prompt behind a cached prefix need (a ring holds the last `slots` positions only).
+ *
+ * k_pages, v_pages [n_pages][n_kv_heads][page_size][head_dim]; position s of sequence b lives in
+ * row s mod page_size of page table[b][s / page_size].  table: int32 [batch][table_width], device
+ * memory.  An entry outside [0, n_pages) is no page: positions it would hold are not stored by an
+ * append and lie outside every support (pages may be dropped, also from the middle of a sequence);
+ * so are positions from table_width * page_size on.  Sequences may share pages that no call of
+ * pbb_paged_append writes at the same time.
+ *
+ * Tokens of a call are packed: sequence b brings rows q_start[b] .. q_start[b+1] - 1 of the packed
+ * tensors, token i of them at position pos[b] + i.  q_start: int32 [batch + 1], device memory,
+ * 0 <= q_start[b] <= q_start[b+1] <= n_tokens (entries beyond are cut to that range, so that no
+ * access leaves a buffer; where they fall, rows are computed for either sequence or not at all);
+ * NULL: every sequence brings n_tokens / batch tokens (n_tokens a multiple of batch; a decode step
+ * has n_tokens = batch).  Rows before q_start[0] or from q_start[batch] on are left as they are.  A
+ * negative pos[b], or one above 2^31 - 1 - n_tokens, skips the sequence: its rows of q_out and out
+ * become zero, lse -inf, nothing is appended.
+ *
+ * Constraints (PBB_ERR_SHAPE otherwise): batch >= 1; heads and head_dim as pbb_desc_t; page_size a
+ * multiple of 16; n_pages >= 1; table_width >= 1; table_width * page_size <= 2^30;
+ * n_q_heads * head_dim <= 2^24; 0 <= n_tokens <= 2^30; block even, window and block >= 0 and not
+ * both set; batch * table_width, and n_q_heads * n_tokens, below 2^40.
+ */
+typedef struct {
+  int32_t batch;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int32_t n_pages;
+  int32_t table_width; /* entries of a sequence's table row */
+  int32_t block;       /* > 0: PBB supports of this block size */
+  int32_t window;      /* > 0: sliding window; both 0: every position up to the token's own */
+  int32_t dtype;       /* a pbb_dtype_t */
+  float scale;         /* <= 0 selects 1/sqrt(head_dim) */
+} pbb_paged_desc_t;
+
+/*
+ * Append a chunk of new tokens of every sequence to the cache, the rotation applied on the way.
+ *   k, v    rows [n_tokens][n_kv_heads][head_dim], tokens k_stride and v_stride ELEMENTS apart (as
+ *           x_stride of pbb_rotate)
+ *   q       optional (q and q_out both or neither): rows [n_tokens][n_q_heads][head_dim], turned
+ *           into q_out [n_tokens][n_q_heads][head_dim] (contiguous; may be q itself if q is too)
+ *   rope    optional: turns k and q (v never); NULL copies them.  rope_pos: int32
+ *           [n_axes][n_tokens], or NULL for the cache position (rope->n_axes 1)
+ * k and v must not overlap the pages.  Both dtypes.  Alignment: tensors 16 bytes, int32 arrays 4.
+ */
+pbb_status_t pbb_paged_append(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
+                              const int32_t *q_start, const int32_t *table,
+                              const pbb_rope_t *rope, const int32_t *rope_pos, const void *q,
+                              int64_t q_stride, void *q_out, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, void *k_pages, void *v_pages,
+                              void *stream);
+
+/*
+ * Workspace bytes pbb_paged_attention needs for calls of up to n_tokens tokens (0 where no walk can
+ * be long enough to be spread over several workgroups).  The first PBB_PAGED_COUNTER_BYTES must be
+ * zero before the first call and every call leaves them zero, so one allocation serves every later
+ * call on one stream, for any descriptor it is large enough for; calls that may run concurrently
+ * (captured graphs among them) need separate workspaces.
+ */
+#define PBB_PAGED_COUNTER_BYTES 16384u
+pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_tokens,
+                                       size_t *bytes);
+
+/*
+ * Attention of the packed tokens over the paged cache, which holds them already
+ * (pbb_paged_append): out_t = softmax over s in A(t) of (q_t . k_s * scale) applied to v_s, t the
+ * token's position, A(t) = {0 .. t}, or A_PBB(t) (Eq.(pbb), h = block / 2), or
+ * {max(0, t - window + 1) .. t}, without positions that have no page.  Query head i reads KV head
+ * floor(i / G).  Single tokens, chunks and a mixture of both in one launch.
+ *   q, out   [n_tokens][n_q_heads][head_dim], tokens of q q_stride ELEMENTS apart
+ *   lse      optional float32 [n_q_heads][n_tokens]: log sum_{s in A(t)} e^{z_s}, natural log
+ * A token with an empty support (every page dropped) gets a zero output and lse -inf.  What cached
+ * rows outside a token's support hold (NaN and infinities included) does not reach its output.
+ * float32: fp32 arithmetic throughout; bfloat16: fp32 accumulation, weights rounded to bf16 for the
+ * value products, output RNE.  workspace: pbb_paged_workspace_bytes bytes, 16-byte aligned (NULL if
+ * 0; PBB_ERR_WORKSPACE if NULL or smaller otherwise).  out must not overlap an input.
+ */
+pbb_status_t pbb_paged_attention(const pbb_paged_desc_t *desc, int32_t n_tokens,
+                                 const int32_t *pos, const int32_t *q_start, const int32_t *table,
+                                 const void *q, int64_t q_stride, const void *k_pages,
+                                 const void *v_pages, void *out, float *lse, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,8 +1,9 @@
 """Build libpbb.so in-tree with hipcc for gfx950.
 
 ``python -m paper_2606_02680_amd.build`` compiles ``csrc/pbb_api.cpp``,
-``csrc/pbb_kernels.hip`` (decode), ``csrc/pbb_prefill.hip`` (prefill) and
-``csrc/pbb_backward.hip`` (training backward) into ``paper_2606_02680_amd/libpbb.so`` (and the
+``csrc/pbb_kernels.hip`` (decode), ``csrc/pbb_prefill.hip`` (prefill),
+``csrc/pbb_backward.hip`` (training backward), ``csrc/pbb_paged_api.cpp``, ``csrc/pbb_rotary.hip``
+(rotary rows, paged append) and ``csrc/pbb_paged*.hip`` (attention over a paged cache) into ``paper_2606_02680_amd/libpbb.so`` (and the
 streaming-read probe ``csrc/pbb_probe.hip``, a measurement helper, into ``libpbbprobe.so``) and
 writes the compiler's
 per-kernel resource report (VGPRs, AGPRs, SGPRs, LDS, scratch) to ``_build/resource_usage.txt``
@@ -21,6 +22,9 @@ LIB = os.path.join(PKG, "libpbb.so")
 PROBE_LIB = os.path.join(PKG, "libpbbprobe.so")   # measurement helper (include/pbb_probe.h)
 ARCH = "gfx950"
 
+SOURCES = ("pbb_api.cpp", "pbb_kernels.hip", "pbb_prefill.hip", "pbb_backward.hip",
+           "pbb_paged_api.cpp", "pbb_rotary.hip", "pbb_paged.hip", "pbb_paged_f32.hip")
+
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
     # Keep the compiler from emitting packed fp32 arithmetic (v_pk_fma_f32 and friends).
@@ -37,8 +41,7 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    sources = [os.path.join(CSRC, "pbb_api.cpp"), os.path.join(CSRC, "pbb_kernels.hip"),
-               os.path.join(CSRC, "pbb_prefill.hip"), os.path.join(CSRC, "pbb_backward.hip")]
+    sources = [os.path.join(CSRC, name) for name in SOURCES]
     tmp = LIB + ".tmp"
     cmd = [hipcc(), *HIPCC_FLAGS, "-Rpass-analysis=kernel-resource-usage", *sources, "-o", tmp]
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "pbb_paged_index.h"
+
 namespace pbb {
 
 enum SupportMode : int32_t { kSupportPBB = 0, kSupportSWA = 1 };
@@ -109,6 +111,83 @@ struct BackwardArgs {
   float scale_log2;    // scale times log2(e)
 };
 
+// Rotary rates of a launch (pbb_rope_t, checked).
+struct RopeArgs {
+  double turns[64];
+  uint8_t axis[64];
+};
+
+// Rotation of rows, validated on the host; n >= 1.  Strides in bytes.
+struct RotateArgs {
+  const void* x;
+  void* out;
+  const int32_t* positions;   // [axes][n]
+  int64_t x_stride, out_stride;
+  int32_t n;
+  int32_t heads;
+  int32_t run;                // heads per grid row (set by the launcher)
+  RopeArgs rope;              // negative rates turn backwards
+};
+
+// Append to a paged cache, validated on the host; n >= 1.  Strides in bytes.
+struct AppendArgs {
+  const int32_t* pos;
+  const int32_t* q_start;     // null with uniform >= 0
+  const int32_t* table;
+  const int32_t* rope_pos;    // null: the cache position
+  const void* q;              // null: no queries
+  void* q_out;
+  const void* k;
+  const void* v;
+  void* k_pages;
+  void* v_pages;
+  int64_t q_stride, k_stride, v_stride;
+  int32_t n;
+  int32_t batch;
+  int32_t uniform;            // tokens of every sequence, -1: q_start says
+  int32_t hq;
+  int32_t hkv;
+  int32_t run;                // rows per grid row (set by the launcher)
+  int32_t turn;               // 1: rope applies
+  FastDiv by_uniform;
+  PagedShape shape;
+  RopeArgs rope;
+};
+
+// Attention over a paged cache, validated on the host; n >= 1.
+struct PagedArgs {
+  const int32_t* pos;
+  const int32_t* q_start;     // null with plan.uniform >= 0
+  const int32_t* table;
+  const void* q;              // rows [n][hq][d], tokens q_stride bytes apart
+  const void* k_pages;        // [n_pages][hkv][page_size][d]
+  const void* v_pages;
+  void* out;                  // [n][hq][d]
+  float* lse;                 // optional [hq][n]
+  uint32_t* counters;         // per partial state of a head, zero between launches
+  float* states;              // partial states of cut walks
+  int64_t q_stride;
+  int32_t n;
+  int32_t batch;
+  int32_t hq;
+  int32_t hkv;
+  int32_t group;
+  float scale_log2;
+  PagedShape shape;
+  PagedPlan plan;
+};
+
+// Query columns (tokens of a tile times the heads of a group) and keys per step of the paged
+// attention kernels.
+constexpr int kPagedCols = 128, kPagedStep = 32;          // bf16
+constexpr int kPagedColsF32 = 64, kPagedStepF32 = 16;     // fp32
+constexpr size_t kPagedCounterBytes = 16384;
+
+// Bytes of one partial state: an unnormalised output, a reference and a sum per column.
+constexpr size_t paged_state_bytes(int cols, int head_dim) {
+  return (size_t)cols * (size_t)(head_dim + 2) * 4;
+}
+
 hipError_t launch_ring_zero(void* k_ring, void* v_ring, size_t bytes_per_tensor,
                             hipStream_t stream);
 
@@ -128,6 +207,12 @@ hipError_t launch_backward_bf16(const BackwardArgs& a, int32_t head_dim, hipStre
 
 // fp32 decode, on matrix cores (one query head per KV head: on vector ALUs); head_dim 64 or 128.
 hipError_t launch_decode_f32(const DecodeArgs& a, int32_t head_dim, hipStream_t stream);
+
+// Rotary rows, paged append, attention over a paged cache; head_dim 64 or 128.
+hipError_t launch_rotate(const RotateArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
+hipError_t launch_paged_append(const AppendArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
+hipError_t launch_paged_bf16(const PagedArgs& a, int32_t head_dim, hipStream_t stream);
+hipError_t launch_paged_f32(const PagedArgs& a, int32_t head_dim, hipStream_t stream);
 
 // The library-held decode workspace of the current device (kNoAllocScratchBytes bytes): its
 // device address, resolved once per device, whose first call also clears the counter block

@@ -1,0 +1,474 @@
+// bf16 attention over a paged KV cache on gfx950 (MI355X): chunks of new tokens, or single ones.
+//
+// A target at position t attends with one softmax over its support {a(t) .. t} (a(t) = 0, or that of
+// the PBB or sliding-window layer), whose keys lie in pages of 16 n rows that a table names.
+//
+// Work unit: a tile of TQ = floor(128 / G) consecutive tokens of one sequence with the G query heads
+// of a KV head, up to 128 query columns, position-major, head-minor; 32 columns per wave in two
+// groups of 16.  The keys of the tile's walk stream through LDS in 32-key steps by LDS DMA, each
+// loaded once per workgroup: wave w loads 16 rows of K or V, which lie in one page, so a step costs a
+// wave one table entry, read through the scalar cache a step ahead.  S^T = K Q^T and O^T += V^T P^T on
+// v_mfma_f32_16x16x32_bf16, with an online softmax whose reference moves lazily, as in the prefill.
+// Long walks are cut into pieces (PagedPlan), which leave partial states (Eq.(lse)) that the last of
+// them to end merges.
+//
+// Masks.  Steps with a key outside some column's support set its scores to -inf.  What such keys hold
+// is unknown (rows never written, dropped pages), and 0 * inf or 0 * NaN would reach the products, so
+// masked steps look whether any value that they read is infinite or NaN, and if so take them apart:
+// finite values enter the product, the others only the columns that see their key.
+
+#include "pbb_paged_device.h"
+
+namespace pbb {
+namespace {
+
+constexpr int kPagedWaves = 4;
+constexpr int kPagedGroups = 2;
+static_assert(kPagedCols == 16 * kPagedGroups * kPagedWaves && kPagedStep == 32, "tile");
+// LDS stages and waves per SIMD that the registers are budgeted for (see the prefill).
+constexpr int kPagedStages128 = 3, kPagedOcc128 = 3;
+constexpr int kPagedStages64 = 4, kPagedOcc64 = 4;
+// Starting reference of the running maximum (log2 units): finite and below any score.
+constexpr float kNoScore = -3.0e38f;
+
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+
+// Whether one of the bf16 values of an operand is infinite or NaN.
+template <int N>
+__device__ __forceinline__ bool any_special(const u32x2 (&v)[N]) {
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[i][e] & 0x7FFF7FFFu));
+  return top[0] >= 0x7F80 || top[1] >= 0x7F80;
+}
+
+// A word of two bf16 values: finite ones (others 0), and 1.0 for each that is +inf or NaN (SIGN 0),
+// or -inf or NaN (SIGN 1).
+__device__ __forceinline__ uint32_t special_halves(uint32_t w) {
+  return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
+         ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+template <int SIGN>
+__device__ __forceinline__ uint32_t ones_where(uint32_t w) {
+  auto half = [](uint32_t h) -> uint32_t {
+    const bool special = (h & 0x7F80u) == 0x7F80u, nan = special && (h & 0x7Fu) != 0;
+    return special && (nan || (h >> 15) == (uint32_t)SIGN) ? 0x3F80u : 0u;
+  };
+  return half(w & 0xFFFFu) | (half(w >> 16) << 16);
+}
+
+template <int D, int ST, int OCC>
+__global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_eu(OCC)))
+void paged_bf16_kernel(PagedArgs a) {
+  constexpr int NW = kPagedWaves;
+  constexpr int QC = kPagedGroups;
+  constexpr int KK = D / 32;            // 32-channel slices of the score contraction
+  constexpr int NB = D / 16;            // 16-channel blocks of the output
+  constexpr int ROWB = D * 2;           // bytes of one K or V row
+  constexpr int HALF = 16 * ROWB;       // 16 rows of a tile
+  constexpr int TILE = 2 * HALF;
+  constexpr int BUF = 2 * TILE;         // K tile, then V tile
+  constexpr int STAGES = ST;
+  static_assert(STAGES >= 3, "stages");
+  static_assert(NW == 4, "one (tensor, 16-row half) of a step per wave");
+  __shared__ __align__(1024) unsigned char smem[STAGES * BUF];
+  __shared__ int last_one;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15;
+  const int j4 = lane >> 4;
+  const int G = a.group;
+  const PagedPlan& pl = a.plan;
+  const PagedShape& sh = a.shape;
+
+  const int item = pl.by_hkv.div((int)blockIdx.x);
+  const int g = (int)blockIdx.x - item * a.hkv;
+  PagedItem it;
+  if (!find_item(a, item, lane, it)) return;
+  const int p0 = it.tile * pl.tq;                               // the tile's tokens in the chunk
+  const int tokens = min(pl.tq, it.c.count - p0);
+  const int64_t row0 = (int64_t)it.c.row0 + p0;                 // packed row of the first one
+  const int cols = tokens * G;
+
+  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
+    if (it.piece > 0) return;
+    for (int i = tid; i < cols * (ROWB / 16); i += NW * 64) {
+      const int col = i / (ROWB / 16), pc = i - col * (ROWB / 16);
+      const int cp = pl.by_group.div(col);
+      *(u32x4*)((unsigned char*)a.out + ((row0 + cp) * a.hq + (int64_t)g * G + (col - cp * G)) * ROWB +
+                pc * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+    if (a.lse != nullptr)
+      for (int col = tid; col < cols; col += NW * 64) {
+        const int cp = pl.by_group.div(col);
+        a.lse[(int64_t)(g * G + col - cp * G) * a.n + row0 + cp] = kNegInf;
+      }
+    return;
+  }
+
+  const int t0 = it.c.pos + p0;
+  const int t_last = t0 + tokens - 1;
+  int s_first = sh.support_lo(t0) >> 5;
+  int nsteps = max(0, (min(t_last, sh.capacity - 1) >> 5) - s_first + 1);
+  if (it.ways > 1) {
+    const int lo = (int)((int64_t)it.piece * nsteps / it.ways);
+    const int hi = (int)((int64_t)(it.piece + 1) * nsteps / it.ways);
+    s_first += lo;
+    nsteps = hi - lo;
+  }
+
+  // This lane's query columns: column col -> token p0 + col / G, head g*G + col % G.  Columns past
+  // the tile's tokens get zero queries and see no key of a masked step (tcol -1); they load the last
+  // token's row, and nothing of them is stored.
+  struct Column {
+    int cp, head;   // token within the tile (the last one for columns past it), query head
+    bool valid;
+  };
+  auto column = [&](int qc, int c) -> Column {
+    const int col = (wave * QC + qc) * 16 + c;
+    const int cp = pl.by_group.div(col);
+    const int cu = min(cp, tokens - 1);
+    return Column{cu, col - cp * G, cp == cu};
+  };
+  int tcol[QC], lo_c[QC];
+  bf16x8 qB[QC][KK];
+#pragma unroll
+  for (int qc = 0; qc < QC; ++qc) {
+    const Column x = column(qc, c16);
+    tcol[qc] = x.valid ? t0 + x.cp : -1;
+    lo_c[qc] = sh.support_lo(t0 + x.cp);
+    const unsigned char* qrow = (const unsigned char*)a.q + (row0 + x.cp) * a.q_stride +
+                                (int64_t)(g * G + x.head) * ROWB + 16 * j4;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qB[qc][kk] = *(const bf16x8*)(qrow + 64 * kk);
+  }
+
+  // DMA of a step: wave w loads 16 rows (half w & 1) of K (w < 2) or V from the page that holds
+  // them.  An entry that names no page reads page 0, and the half's keys are masked (`gone`, two
+  // bits per step, the youngest lowest).
+  const unsigned char* const pool = (const unsigned char*)(wave >= 2 ? a.v_pages : a.k_pages);
+  const int32_t* const table = a.table + (size_t)it.b * sh.width;
+  int next_key = s_first * 32;   // first key of the step to be issued next
+  int id0 = 0, id1 = 0;          // its entries (the two halves')
+  auto fetch = [&]() {
+    const int i0 = sh.by_page.div(next_key), i1 = sh.by_page.div(next_key + 16);
+    id0 = i0 < sh.width ? scalar_word(table, i0) : -1;
+    id1 = i1 < sh.width ? scalar_word(table, i1) : -1;
+  };
+  uint32_t gone = 0;
+  uint32_t doff[kDmaBlocks<D>];
+  dma_offsets<D>(lane, ROWB, doff);
+  auto issue = [&](int stage) {   // the next step
+    gone |= (sh.is_page(id0) ? 0u : 1u) | (sh.is_page(id1) ? 0u : 2u);
+    const int key = next_key + 16 * (wave & 1);
+    const int id = (wave & 1) ? id1 : id0;
+    const int slot = key - sh.by_page.div(key) * sh.page_size;
+    const unsigned char* src =
+        pool + (((size_t)(sh.is_page(id) ? id : 0) * a.hkv + g) * sh.page_size + slot) * ROWB;
+    unsigned char* lds = smem + stage * BUF + wave * HALF;
+#pragma unroll
+    for (int y = 0; y < 2 * kDmaBlocks<D>; ++y)
+      dma16(y < kDmaBlocks<D> ? src : src + 8 * ROWB, doff[y % kDmaBlocks<D>], lds + 1024 * y);
+    next_key += 32;
+    fetch();
+  };
+  fetch();
+
+  // Steps 0 .. STAGES-2 go out first; step st then issues step st + STAGES - 1.
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    gone <<= 2;
+    if (s < nsteps) issue(s);
+  }
+
+  // LDS byte addresses of this lane's reads in stage 0 (tile_addresses; the V tile is TILE on).
+  uint32_t ra[2], va[4];
+  {
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    tile_addresses<D>(base, c16, j4, ra, va);
+  }
+  const __attribute__((address_space(3))) unsigned char* lds0 = nullptr;
+
+  // The wave's own range of steps [wlo, whi] (its columns' positions tw_lo .. tw_hi), and the
+  // run [ua, ub) of them whose keys all lie in every column's support (a(t) never decreases).
+  const int w_first = pl.by_group.div(wave * 16 * QC);
+  const int tw_lo = t0 + min(w_first, tokens - 1);
+  const int tw_hi = t0 + min(pl.by_group.div(wave * 16 * QC + 16 * QC - 1), tokens - 1);
+  const int wlo = w_first < tokens ? max(0, (sh.support_lo(tw_lo) >> 5) - s_first) : nsteps;
+  const int whi = min(nsteps - 1, (tw_hi >> 5) - s_first);
+  const int ua = ((sh.support_lo(tw_hi) + 31) >> 5) - s_first;
+  const int ub = ((tw_lo + 1) >> 5) - s_first;
+
+  // m starts at a finite floor below any score, so that a column whose keys are all masked so
+  // far gets exp2(-inf - m) = 0 without a separate test; its first real maximum always moves m.
+  // Columns past the tile's tokens score 0 against a reference of 0: they never move it.
+  float m[QC], lsum[QC];
+  f32x4 acc[QC][NB];
+#pragma unroll
+  for (int qc = 0; qc < QC; ++qc) {
+    m[qc] = tcol[qc] >= 0 ? kNoScore : 0.0f;
+    lsum[qc] = 0.0f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[qc][nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qB[qc][kk] = __builtin_bit_cast(
+          bf16x8, tcol[qc] >= 0 ? __builtin_bit_cast(u32x4, qB[qc][kk]) : u32x4{0u, 0u, 0u, 0u});
+  }
+  const float sc = a.scale_log2;
+
+  int rstage = 0;
+  constexpr int OPS = D / 32;           // DMA instructions of a wave per step
+
+  // Begins step st: its tiles have landed; returns the stage offset.
+  auto begin_step = [&](int st) -> uint32_t {
+    // This wave's loads of step st have landed once at most the loads of the steps issued
+    // after it (up to STAGES - 2) are outstanding; the barrier then covers every wave's loads,
+    // and every wave is done with step st-1, whose stage the loads of step st+STAGES-1 reuse.
+    wait_groups<STAGES - 2, OPS>(min(STAGES - 2, nsteps - 1 - st));
+    lds_barrier();
+    gone <<= 2;
+    if (st + STAGES - 1 < nsteps) issue(rstage == 0 ? STAGES - 1 : rstage - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    const uint32_t sb = (uint32_t)(rstage * BUF);
+    rstage = rstage == STAGES - 1 ? 0 : rstage + 1;
+    return sb;
+  };
+
+  auto step = [&](int st, uint32_t sb) {
+    f32x4 s0[QC], s1[QC];
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+      s0[qc] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      s1[qc] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const auto* kp = lds0 + ra[kk & 1] + sb + kTileLine * (kk >> 1);
+      const bf16x8 ka = *(const __attribute__((address_space(3))) bf16x8*)(kp);
+      const bf16x8 kb = *(const __attribute__((address_space(3))) bf16x8*)(kp + HALF);
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc) {
+        s0[qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qB[qc][kk], s0[qc], 0, 0, 0);
+        s1[qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qB[qc][kk], s1[qc], 0, 0, 0);
+      }
+    }
+    // Element e of s0 is key k0 + 4 j4 + e of the lane's column, of s1 key k0 + 16 + 4 j4 + e.
+    const uint32_t dropped = (gone >> (2 * (STAGES - 1))) & 3u;
+    const bool masked = st < ua || st >= ub || dropped != 0;
+    const int k0 = (s_first + st) * 32 + 4 * j4;
+    auto seen = [&](int qc, int e) -> bool {   // element e: 0..3 of s0, 4..7 of s1
+      const int k = e < 4 ? e : e + 12;
+      return k >= lo_c[qc] - k0 && k <= tcol[qc] - k0 && !(dropped & (e < 4 ? 1u : 2u));
+    };
+    if (masked) {
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s0[qc][e] = seen(qc, e) ? s0[qc][e] : kNegInf;
+          s1[qc][e] = seen(qc, 4 + e) ? s1[qc][e] : kNegInf;
+        }
+    }
+    // Online softmax in log2 units with a lazily moved reference m (the log-sum-exp rescaling
+    // of Eq.(lse)): the weights are taken against the current m, and m moves to the column
+    // maxima (the accumulators rescaled, the weights taken again) only in a step where the
+    // eight weights of some lane and column sum above 2^8 or to infinity.
+    bf16x8 pB[QC];
+    float ps[QC];
+    auto weights = [&]() {
+      bool over = false;
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float pe =
+              fast_exp2(__builtin_fmaf(e < 4 ? s0[qc][e] : s1[qc][e - 4], sc, -m[qc]));
+          sum += pe;
+          pB[qc][e] = (__bf16)pe;
+        }
+        ps[qc] = sum;
+        over |= !(sum <= kWeightCap);
+      }
+      return over;
+    };
+    auto column_max = [&](int qc) {
+      float mx = kNegInf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, e < 4 ? s0[qc][e] : s1[qc][e - 4]);
+      return max_xor16_32(mx) * sc;
+    };
+    // The wave's first step sets the reference before its weights (it would always move it);
+    // its sums and accumulators are still zero.
+    if (st == wlo) {
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc) m[qc] = fmaxf(m[qc], column_max(qc));
+    }
+    // V^T operand of O^T += V^T P^T: lane (c16, j4) needs channel 16nb + c16 of keys
+    // 4j4..4j4+3 and 16+4j4..16+4j4+3 (the key order of P^T in the score layout): one transposed
+    // read per half.
+    u32x2 vr[2 * NB];
+    if (__builtin_amdgcn_ballot_w64(weights()) != 0) {
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc) {
+        const float cand = column_max(qc);
+        // (only the columns whose own weights ask for it: none depends on its neighbours' data)
+        const bool grow = cand > m[qc] && max_xor16_32(ps[qc]) > kWeightCap;
+        const float alpha = grow ? fast_exp2(m[qc] - cand) : 1.0f;
+        m[qc] = grow ? cand : m[qc];
+        lsum[qc] *= alpha;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[qc][nb] *= alpha;
+      }
+      weights();
+    }
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) lsum[qc] += ps[qc];
+    read_chunks<D, TILE>(vr, va, sb);
+    wait_chunks<D>(vr);
+    if (masked && __builtin_amdgcn_ballot_w64(any_special(vr)) != 0) {
+      // Infinities and NaN among the step's values: 1 for each that is +inf or NaN (-inf or NaN),
+      // times 1 for each key that the column sees, counts those that a column's output takes.
+      bf16x8 one[QC];
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) one[qc][e] = seen(qc, e) ? (__bf16)1.0f : (__bf16)0.0f;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        u32x2 up[2], down[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t w = vr[2 * nb + i][e];
+            up[i][e] = ones_where<0>(w);
+            down[i][e] = ones_where<1>(w);
+            vr[2 * nb + i][e] = w & ~special_halves(w);
+          }
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+          const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+          const f32x4 cu = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join_chunks(up[0], up[1]), one[qc],
+                                                                   z, 0, 0, 0);
+          const f32x4 cd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join_chunks(down[0], down[1]),
+                                                                   one[qc], z, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[qc][nb][e] += (cu[e] > 0.0f ? -kNegInf : 0.0f) + (cd[e] > 0.0f ? kNegInf : 0.0f);
+        }
+      }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const bf16x8 vt = join_chunks(vr[2 * nb], vr[2 * nb + 1]);
+#pragma unroll
+      for (int qc = 0; qc < QC; ++qc)
+        acc[qc][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pB[qc], acc[qc][nb], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  int st = 0;
+  for (; st < wlo && st < nsteps; ++st) begin_step(st);
+  for (; st <= whi; ++st) {
+    const uint32_t sb = begin_step(st);
+    step(st, sb);
+  }
+  for (; st < nsteps; ++st) begin_step(st);
+
+  // Output of a column: o = acc / l (bf16 RNE), lse = (m + log2 l) * ln 2; an empty support has l 0
+  // and gets zeros and -inf.
+  auto inverse = [](float l) { return l == 0.0f ? 0.0f : 1.0f / l; };
+  auto log_partition = [](float mref, float l) {
+    return l == 0.0f ? kNegInf : (mref + __builtin_log2f(l)) * 0.69314718055994531f;
+  };
+  if (it.ways == 1) {
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+      const float l = sum_xor16_32(lsum[qc]);
+      const float inv = inverse(l);
+      u32x4 w[NB / 2];
+#pragma unroll
+      for (int q = 0; q < NB / 2; ++q) w[q] = pair_blocks(acc[qc][2 * q], acc[qc][2 * q + 1], inv);
+      const Column x = column(qc, c16);
+      if (x.valid) {
+        unsigned char* orow = (unsigned char*)a.out +
+                              ((row0 + x.cp) * a.hq + (int64_t)(g * G + x.head)) * ROWB;
+#pragma unroll
+        for (int q = 0; q < NB / 2; ++q)
+          *(u32x4*)(orow + 64 * q + 32 * (j4 & 1) + 16 * (j4 >> 1)) = w[q];
+        if (a.lse != nullptr && j4 == 0)
+          a.lse[(int64_t)(g * G + x.head) * a.n + row0 + x.cp] = log_partition(m[qc], l);
+      }
+    }
+    return;
+  }
+
+  // A cut walk: the piece's state, device-coherent, then the count of the tile's pieces; whoever
+  // completes it merges them (coherent_store2 says why this orders).
+  constexpr size_t STATE = paged_state_bytes(kPagedCols, D) / 4;
+  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
+  float* const part = a.states + (unit + it.piece) * STATE;
+#pragma unroll
+  for (int qc = 0; qc < QC; ++qc) {
+    const float l = sum_xor16_32(lsum[qc]);
+    const int col = (wave * QC + qc) * 16 + c16;
+    if (col < cols) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        coherent_store2(part + col * D + 16 * nb + 4 * j4, acc[qc][nb][0], acc[qc][nb][1]);
+        coherent_store2(part + col * D + 16 * nb + 4 * j4 + 2, acc[qc][nb][2], acc[qc][nb][3]);
+      }
+      if (j4 == 0) coherent_store2(part + kPagedCols * D + 2 * col, m[qc], l);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+    last_one = before == (unsigned)(it.ways - 1);
+    if (last_one)
+      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!last_one) return;
+  auto address = [&](int col) -> int64_t {
+    const int cp = pl.by_group.div(col);
+    return (row0 + cp) * a.hq + (int64_t)(g * G + col - cp * G);
+  };
+  merge_states<D, kPagedCols, NW * 64>(
+      a.states + unit * STATE, STATE, it.ways, cols, tid,
+      [&](int col, int c, f32x4 o, float l) {
+        const float inv = inverse(l);
+        *(u32x2*)((unsigned char*)a.out + address(col) * ROWB + 2 * c) =
+            u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+      },
+      [&](int col, float mref, float l) {
+        if (a.lse == nullptr) return;
+        const int cp = pl.by_group.div(col);
+        a.lse[(int64_t)(g * G + col - cp * G) * a.n + row0 + cp] = log_partition(mref, l);
+      });
+}
+
+}  // namespace
+
+hipError_t launch_paged_bf16(const PagedArgs& a, int32_t head_dim, hipStream_t stream) {
+  const unsigned blocks = (unsigned)(a.plan.items() * a.hkv);
+  if (head_dim == 64)
+    hipLaunchKernelGGL((paged_bf16_kernel<64, kPagedStages64, kPagedOcc64>), dim3(blocks),
+                       dim3(kPagedWaves * 64), 0, stream, a);
+  else
+    hipLaunchKernelGGL((paged_bf16_kernel<128, kPagedStages128, kPagedOcc128>), dim3(blocks),
+                       dim3(kPagedWaves * 64), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace pbb

@@ -1,0 +1,135 @@
+// Index arithmetic of the paged-cache launches, usable on the host and in kernels (and by a plain
+// C++ compiler: nothing here needs HIP).
+#pragma once
+
+#include <stdint.h>
+
+#include "pbb_index.h"
+
+namespace pbb {
+
+enum PagedSupport : int32_t { kPagedFull = 0, kPagedPBB = 1, kPagedSWA = 2 };
+
+// Rows and positions of one sequence's chunk in a packed call.
+struct Chunk {
+  int row0;    // first packed row
+  int count;   // tokens (0: none)
+  int pos;     // position of the first one; negative: the sequence is skipped
+};
+
+// A sequence's chunk from its q_start entries (or, uniform >= 0, that many tokens each) and pos,
+// cut so that no row leaves [0, n_tokens) and no position passes 2^31 - 1.
+PBB_HD Chunk chunk_of(int b, int uniform, int start, int end, int pos, int n_tokens) {
+  Chunk c;
+  if (uniform >= 0) {
+    c.row0 = b * uniform;
+    c.count = uniform;
+  } else {
+    const int s = start < 0 ? 0 : start > n_tokens ? n_tokens : start;
+    const int e = end < s ? s : end > n_tokens ? n_tokens : end;
+    c.row0 = s;
+    c.count = e - s;
+  }
+  c.pos = pos > 0x7fffffff - n_tokens ? -1 : pos;
+  return c;
+}
+
+// Everything a walk over a cache depends on, launch constants.
+struct PagedShape {
+  int page_size, n_pages, width;
+  int capacity;          // width * page_size: positions from here on have no page
+  int support;           // PagedSupport
+  int half, window;      // PBB: half-block; sliding window
+  FastDiv by_page, by_half;
+  static PagedShape make(int page_size, int n_pages, int width, int block, int window) {
+    PagedShape s;
+    s.page_size = page_size;
+    s.n_pages = n_pages;
+    s.width = width;
+    s.capacity = page_size * width;
+    s.support = block > 0 ? kPagedPBB : window > 0 ? kPagedSWA : kPagedFull;
+    s.half = block / 2;
+    s.window = window;
+    s.by_page = FastDiv::make((uint32_t)page_size);
+    s.by_half = FastDiv::make((uint32_t)(block > 0 ? block / 2 : 1));
+    return s;
+  }
+  // First source of the support of target t; never decreases in t.
+  PBB_HD int support_lo(int t) const {
+    const int lo = support == kPagedFull ? 0
+                   : support == kPagedPBB ? half * (by_half.div(t) - 1)
+                                          : t - window + 1;
+    return lo > 0 ? lo : 0;
+  }
+  // A table entry, made safe to address with: 0 in place of one that names no page.
+  PBB_HD bool is_page(int id) const { return (uint32_t)id < (uint32_t)n_pages; }
+  // Keys that a run of `tokens` targets ending at position `last` can walk, at most.
+  PBB_HD int64_t max_keys(int last, int tokens) const {
+    const int64_t all = (int64_t)(last < capacity ? last + 1 : capacity);
+    const int64_t span = support == kPagedPBB   ? 2 * (int64_t)half + tokens
+                         : support == kPagedSWA ? (int64_t)window + tokens
+                                                : all;
+    return span < all ? span : all;
+  }
+};
+
+// How the walks of an attention call are spread over workgroups.
+//
+// A unit is a tile of `tq` tokens of one sequence under one KV head; its walk is a number of key
+// steps.  With T the call's steps per KV head (tiles times the sequence's longest walk) and a
+// budget of `pieces` workgroups per KV head, a sequence's walks are cut into P = ceil(steps / C)
+// pieces each, C = max(least, T / pieces): so no piece is longer than an even share of the whole
+// (a sequence far longer than the others does not hold the call up), there are at most
+// tiles + pieces workgroups, and at most 2 x pieces of them belong to walks that are cut.  The
+// kernels work this out by themselves, from positions that only the device knows.
+constexpr int kPagedPieces = 1024;   // workgroups that a call's cut walks may add, in all heads
+constexpr int kPagedLeastSteps = 8;  // key steps of a piece, at least
+
+struct PagedPlan {
+  int tq;        // tokens per tile
+  int step;      // keys per step
+  int pieces;    // budget per KV head; 0: no walk is cut
+  int uniform;   // tokens of every sequence, -1: q_start says
+  int tiles;     // tiles of a call, at most
+  int slots;     // partial states per KV head, at most
+  FastDiv by_hkv, by_tq, by_group;
+  static PagedPlan make(const PagedShape& s, int batch, int hkv, int group, int n_tokens,
+                        bool ragged, int cols, int step) {
+    PagedPlan p;
+    p.tq = cols / group;
+    p.step = step;
+    p.uniform = ragged ? -1 : n_tokens / batch;
+    p.by_hkv = FastDiv::make((uint32_t)hkv);
+    p.by_tq = FastDiv::make((uint32_t)p.tq);
+    p.by_group = FastDiv::make((uint32_t)group);
+    // ceil(n / tq) of every sequence, summed: at most one more each than of all together
+    p.tiles = ragged ? n_tokens / p.tq + (batch < n_tokens ? batch : n_tokens)
+                     : batch * ((p.uniform + p.tq - 1) / p.tq);
+    const int64_t keys = s.max_keys(s.capacity, p.tq);
+    const int64_t longest = (keys + step - 1) / step + 1;
+    p.pieces = longest > kPagedLeastSteps && 2 * hkv <= kPagedPieces ? kPagedPieces / hkv : 0;
+    p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
+    return p;
+  }
+  // Tiles of a chunk, and the longest walk of one of them in steps.
+  PBB_HD int tiles_of(const Chunk& c) const { return c.count > 0 ? by_tq.div(c.count - 1) + 1 : 0; }
+  PBB_HD int steps_of(const PagedShape& s, const Chunk& c) const {
+    if (c.pos < 0 || c.count == 0) return 1;
+    const int64_t keys = s.max_keys(c.pos + c.count - 1, tq < c.count ? tq : c.count);
+    return (int)((keys + step - 1) / step) + 1;
+  }
+  // Pieces of each of a sequence's walks, share = the steps C of a piece.
+  PBB_HD int pieces_of(int steps, float share) const {
+    if (pieces == 0) return 1;
+    const int p = (int)__builtin_ceilf((float)steps / share);
+    return p > 1 ? p : 1;
+  }
+  PBB_HD float share_of(float total) const {
+    const float c = pieces > 0 ? total / (float)pieces : 0.0f;
+    return c > (float)kPagedLeastSteps ? c : (float)kPagedLeastSteps;
+  }
+  // Workgroups per KV head, at most.
+  int64_t items() const { return (int64_t)tiles + pieces + pieces / 16 + 1; }
+};
+
+}  // namespace pbb

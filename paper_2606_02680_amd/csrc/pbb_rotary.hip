@@ -1,0 +1,223 @@
+// Rotary positions and the paged append on gfx950 (MI355X).
+//
+// Channels (c, c + d/2) of a row turn by the angle 2 pi turns[c] p, p the token's position on the
+// pair's axis: (x cos - y sin, y cos + x sin); the transposed rotation, which gradients take, is
+// the same with the angle negated.  The append does this to the new keys (and the chunk's queries)
+// on their way into the pages, and copies the values.
+//
+// Bound: HBM (each row read once and written once).  A lane takes the 16-byte piece of channels
+// c.. and its partner d/2 further on, of the rows of one token that are 64 / PC apart (PC pieces per
+// half row), so a wave reads 64 / PC whole rows at once and works out its sines and cosines once for
+// all rows of the token that it visits.
+
+#include "pbb_device.h"
+#include "pbb_internal.h"
+
+namespace pbb {
+namespace {
+
+constexpr int kRotThreads = 256;
+
+template <typename T>
+struct Piece;   // 16 bytes of a row as floats
+template <>
+struct Piece<uint16_t> {
+  static constexpr int N = 8;
+  typedef u32x4 raw;
+  static __device__ __forceinline__ float get(raw r, int e) {
+    return __uint_as_float(e & 1 ? r[e >> 1] & 0xFFFF0000u : r[e >> 1] << 16);
+  }
+  static __device__ __forceinline__ raw put(const float (&f)[N]) {
+    return raw{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]),
+               pack_bf16(f[6], f[7])};
+  }
+};
+template <>
+struct Piece<float> {
+  static constexpr int N = 4;
+  typedef u32x4 raw;
+  static __device__ __forceinline__ float get(raw r, int e) { return __uint_as_float(r[e]); }
+  static __device__ __forceinline__ raw put(const float (&f)[N]) {
+    return raw{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+               __float_as_uint(f[3])};
+  }
+};
+
+// cos and sin of `turns` whole turns.  The angle is reduced to half a turn either way in fp64.
+// bf16: the hardware's sine and cosine (of turns; their error of a few 2^-22 is far below the
+// rounding of the result); fp32: sincospif, whose last-bit error is of the order of the result's.
+template <typename T>
+__device__ __forceinline__ void cos_sin(double turns, float& cs, float& sn) {
+  const float f = (float)(turns - __builtin_rint(turns));
+  if constexpr (sizeof(T) == 2) {
+    cs = __builtin_amdgcn_cosf(f);
+    sn = __builtin_amdgcn_sinf(f);
+  } else {
+    sincospif(2.0f * f, &sn, &cs);
+  }
+}
+
+// The sines and cosines of piece pc of a row (pairs pc N .. + N - 1) at a token's positions;
+// position(axis) reads them.
+template <typename T, typename F>
+__device__ __forceinline__ void piece_turns(const RopeArgs& r, int pc, F&& position,
+                                            float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
+  constexpr int N = Piece<T>::N;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const int c = pc * N + e;
+    cos_sin<T>((double)position(r.axis[c]) * r.turns[c], cs[e], sn[e]);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&cs)[Piece<T>::N],
+                                            const float (&sn)[Piece<T>::N]) {
+  constexpr int N = Piece<T>::N;
+  float ox[N], oy[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    rope_turn(Piece<T>::get(lo, e), Piece<T>::get(hi, e), cs[e], sn[e], ox[e], oy[e]);
+  lo = Piece<T>::put(ox);
+  hi = Piece<T>::put(oy);
+}
+
+// Grid: x = tokens / waves per workgroup, y = runs of a token's heads.
+template <typename T, int D>
+__global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
+  constexpr int PC = D * (int)sizeof(T) / 32;   // pieces per half row
+  constexpr int ROWS = 64 / PC;                 // rows of a wave at a time
+  constexpr int ROWB = D * (int)sizeof(T);
+  const int lane = threadIdx.x & 63;
+  const int64_t tok = (int64_t)blockIdx.x * (kRotThreads / 64) + (threadIdx.x >> 6);
+  if (tok >= a.n) return;
+  const int pc = lane % PC;
+  float cs[Piece<T>::N], sn[Piece<T>::N];
+  piece_turns<T>(a.rope, pc, [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; }, cs, sn);
+  const unsigned char* x = (const unsigned char*)a.x + tok * a.x_stride + pc * 16;
+  unsigned char* o = (unsigned char*)a.out + tok * a.out_stride + pc * 16;
+  const int h1 = min(a.heads, (int)(blockIdx.y + 1) * a.run);
+  for (int h = blockIdx.y * a.run + lane / PC; h < h1; h += ROWS) {
+    const unsigned char* p = x + (size_t)h * ROWB;
+    u32x4 lo = *(const u32x4*)p, hi = *(const u32x4*)(p + ROWB / 2);
+    turn_pieces<T>(lo, hi, cs, sn);
+    unsigned char* w = o + (size_t)h * ROWB;
+    *(u32x4*)w = lo;
+    *(u32x4*)(w + ROWB / 2) = hi;
+  }
+}
+
+// The chunk that packed row `tok` belongs to, or -1: the number of sequences whose rows end at or
+// before it, 64 at a time (every lane of the wave takes part; q_start is non-decreasing).
+__device__ __forceinline__ int sequence_of(const int32_t* q_start, int batch, int tok, int lane) {
+  int b = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    const bool before = b0 + lane < batch && q_start[b0 + lane + 1] <= tok;
+    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+    b += k;
+    if (k < 64) break;
+  }
+  if (b >= batch) return -1;
+  return __builtin_amdgcn_readfirstlane(q_start[b]) <= tok ? b : -1;
+}
+
+// Grid as rotate_kernel, over a token's query rows, key rows and value rows (in this order).
+template <typename T, int D>
+__global__ __launch_bounds__(kRotThreads) void paged_append_kernel(AppendArgs a) {
+  constexpr int PC = D * (int)sizeof(T) / 32;
+  constexpr int ROWS = 64 / PC;
+  constexpr int ROWB = D * (int)sizeof(T);
+  const int lane = threadIdx.x & 63;
+  const int tok = __builtin_amdgcn_readfirstlane(
+      (int)(blockIdx.x * (kRotThreads / 64) + (threadIdx.x >> 6)));
+  if (tok >= a.n) return;
+  const int b = a.uniform >= 0 ? a.by_uniform.div(tok) : sequence_of(a.q_start, a.batch, tok, lane);
+  if (b < 0) return;
+  const Chunk c = chunk_of(b, a.uniform, a.uniform >= 0 ? 0 : a.q_start[b],
+                           a.uniform >= 0 ? 0 : a.q_start[b + 1], a.pos[b], a.n);
+  const bool skip = c.pos < 0;
+  const int t = skip ? 0 : c.pos + (tok - c.row0);
+  // the page row of position t (page -1: none, nothing is stored)
+  int page = -1, slot = 0;
+  if (!skip && t < a.shape.capacity) {
+    const int i = a.shape.by_page.div(t);
+    slot = t - i * a.shape.page_size;
+    const int id = a.table[(size_t)b * a.shape.width + i];
+    page = a.shape.is_page(id) ? id : -1;
+  }
+  const int pc = lane % PC;
+  float cs[Piece<T>::N], sn[Piece<T>::N];
+  if (a.turn)
+    piece_turns<T>(a.rope, pc,
+                   [&](int axis) {
+                     return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : t;
+                   },
+                   cs, sn);
+  const int hq = a.q != nullptr ? a.hq : 0;
+  const int rows = hq + 2 * a.hkv;
+  const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
+  for (int r = blockIdx.y * a.run + lane / PC; r < r1; r += ROWS) {
+    const unsigned char* p;
+    unsigned char* w;
+    if (r < hq) {
+      p = (const unsigned char*)a.q + tok * a.q_stride + (size_t)r * ROWB;
+      w = (unsigned char*)a.q_out + ((size_t)tok * hq + r) * ROWB;
+    } else {
+      const bool key = r < hq + a.hkv;
+      const int h = r - hq - (key ? 0 : a.hkv);
+      p = (key ? (const unsigned char*)a.k + tok * a.k_stride
+               : (const unsigned char*)a.v + tok * a.v_stride) + (size_t)h * ROWB;
+      if (page < 0) continue;
+      w = (unsigned char*)(key ? a.k_pages : a.v_pages) +
+          (((size_t)page * a.hkv + h) * a.shape.page_size + slot) * ROWB;
+    }
+    u32x4 lo = *(const u32x4*)(p + pc * 16), hi = *(const u32x4*)(p + pc * 16 + ROWB / 2);
+    if (a.turn && r < hq + a.hkv) turn_pieces<T>(lo, hi, cs, sn);
+    if (skip) lo = hi = u32x4{0u, 0u, 0u, 0u};
+    *(u32x4*)(w + pc * 16) = lo;
+    *(u32x4*)(w + pc * 16 + ROWB / 2) = hi;
+  }
+}
+
+// Heads per workgroup row of the grid: all of a token's, unless the tokens alone leave the chip
+// short of waves; then as few as a wave takes at once (and no more than 65535 runs).
+int head_run(int tokens, int heads, int rows) {
+  if (tokens >= 4096) return heads;
+  const int least = (heads + 65534) / 65535;
+  return rows > least ? rows : least;
+}
+
+template <typename T, int D>
+hipError_t rotate_t(const RotateArgs& a0, hipStream_t stream) {
+  RotateArgs a = a0;
+  a.run = head_run(a.n, a.heads, 64 / (D * (int)sizeof(T) / 32));
+  const dim3 grid((unsigned)((a.n + kRotThreads / 64 - 1) / (kRotThreads / 64)),
+                  (unsigned)((a.heads + a.run - 1) / a.run));
+  hipLaunchKernelGGL((rotate_kernel<T, D>), grid, dim3(kRotThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t append_t(const AppendArgs& a0, hipStream_t stream) {
+  AppendArgs a = a0;
+  const int rows = (a.q != nullptr ? a.hq : 0) + 2 * a.hkv;
+  a.run = head_run(a.n, rows, 64 / (D * (int)sizeof(T) / 32));
+  const dim3 grid((unsigned)((a.n + kRotThreads / 64 - 1) / (kRotThreads / 64)),
+                  (unsigned)((rows + a.run - 1) / a.run));
+  hipLaunchKernelGGL((paged_append_kernel<T, D>), grid, dim3(kRotThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const RotateArgs& a, int32_t head_dim, bool f32, hipStream_t stream) {
+  if (f32) return head_dim == 64 ? rotate_t<float, 64>(a, stream) : rotate_t<float, 128>(a, stream);
+  return head_dim == 64 ? rotate_t<uint16_t, 64>(a, stream) : rotate_t<uint16_t, 128>(a, stream);
+}
+
+hipError_t launch_paged_append(const AppendArgs& a, int32_t head_dim, bool f32, hipStream_t stream) {
+  if (f32) return head_dim == 64 ? append_t<float, 64>(a, stream) : append_t<float, 128>(a, stream);
+  return head_dim == 64 ? append_t<uint16_t, 64>(a, stream) : append_t<uint16_t, 128>(a, stream);
+}
+
+}  // namespace pbb

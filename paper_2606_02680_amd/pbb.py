@@ -25,7 +25,8 @@ EXPORTS = ("pbb_status_string", "pbb_ring_bytes", "pbb_ring_init", "pbb_ring_fil
            "pbb_workspace_bytes", "pbb_decode_step", "swa_workspace_bytes", "swa_decode_step",
            "pbb_decode_step_advance", "swa_decode_step_advance", "pbb_prefill", "swa_prefill",
            "pbb_backward_workspace_bytes", "pbb_backward", "swa_backward",
-           "pbb_decode_step_noalloc")
+           "pbb_decode_step_noalloc", "pbb_rope_init", "pbb_rotate", "pbb_paged_append",
+           "pbb_paged_workspace_bytes", "pbb_paged_attention")
 
 
 class PbbError(RuntimeError):
@@ -49,6 +50,25 @@ class PbbDesc(ctypes.Structure):
     @property
     def group(self) -> int:
         return self.n_q_heads // self.n_kv_heads
+
+
+class PbbRope(ctypes.Structure):
+    """Mirror of ``pbb_rope_t``."""
+    _fields_ = [("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("turns", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class PbbPagedDesc(ctypes.Structure):
+    """Mirror of ``pbb_paged_desc_t``."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("table_width", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+    @property
+    def torch_dtype(self) -> torch.dtype:
+        return _TORCH_DTYPE[self.dtype]
 
 
 _lib = None
@@ -82,6 +102,13 @@ def load_library(path: str = _LIB_PATH):
     lib.pbb_backward_workspace_bytes.argtypes = [dp, i32, ctypes.POINTER(sz)]
     for fn in ("pbb_backward", "swa_backward"):
         getattr(lib, fn).argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    rp, pp, i64 = ctypes.POINTER(PbbRope), ctypes.POINTER(PbbPagedDesc), ctypes.c_int64
+    lib.pbb_rope_init.argtypes = [rp, i32, ctypes.c_double, i32, ctypes.POINTER(ctypes.c_uint8)]
+    lib.pbb_rotate.argtypes = [rp, i32, i32, vp, vp, i64, vp, i64, i32, i32, vp]
+    lib.pbb_paged_append.argtypes = [pp, i32, vp, vp, vp, rp, vp, vp, i64, vp, vp, i64, vp, i64, vp,
+                                     vp, vp]
+    lib.pbb_paged_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
+    lib.pbb_paged_attention.argtypes = [pp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
     for fn in EXPORTS[1:]:
         getattr(lib, fn).restype = ctypes.c_int
     _lib = lib
@@ -362,3 +389,171 @@ def swa_backward(desc: PbbDesc, q, k, v, out, dout, lse, dq, dk, dv, workspace=N
     """Sliding-window counterpart of :func:`pbb_backward`."""
     return _backward("swa_backward", desc, q, k, v, out, dout, lse, dq, dk, dv, workspace, stream)
 
+
+def make_rope(head_dim: int, base: float, axis=None) -> PbbRope:
+    """Rotary rates ``base ** (-2c / head_dim)`` of channel pairs (c, c + head_dim / 2).  ``axis``:
+    the axis of every pair (head_dim / 2 whole numbers; time, height and width of images and video),
+    or None for one axis throughout."""
+    rope = PbbRope()
+    n_axes, arr = 1, None
+    if axis is not None:
+        axis = [int(x) for x in axis]
+        if len(axis) != head_dim // 2 or min(axis) < 0 or max(axis) > 255:
+            raise ValueError(f"axis: {head_dim // 2} axes, one of each channel pair")
+        n_axes, arr = max(axis) + 1, (ctypes.c_uint8 * len(axis))(*axis)
+    _check("pbb_rope_init", load_library().pbb_rope_init(ctypes.byref(rope), int(head_dim),
+                                                         float(base), n_axes, arr))
+    return rope
+
+
+def _expect_rows(name: str, t: torch.Tensor, shape, dtype) -> int:
+    """Checks packed rows [tokens][heads][d] whose tokens may lie apart; returns their stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: must be a GPU tensor, got {t.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype} != {dtype}")
+    n, heads, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the rows of a token must be contiguous")
+    return t.stride(0) if n > 1 else heads * d
+
+
+def _expect_on(device, **tensors):
+    """Checks that a call's tensors lie on one device, the current one (whose streams it uses)."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def pbb_rotate(rope: PbbRope, positions: torch.Tensor, x: torch.Tensor, out: torch.Tensor,
+               inverse: bool = False, stream=None):
+    """Turn rows ``x`` [tokens][heads][d] by ``positions`` (int32 [axes][tokens], or [tokens] for one
+    axis) into ``out``; ``inverse`` turns gradients back.  Tokens may lie apart (a part of a fused
+    projection buffer); ``out`` may be ``x``."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise ValueError("x: must be [tokens][heads][d]")
+    n, heads, _ = x.shape
+    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}.get(x.dtype, -1)
+    shape = (n, heads, rope.head_dim)
+    xs, os_ = _expect_rows("x", x, shape, x.dtype), _expect_rows("out", out, shape, x.dtype)
+    if rope.n_axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1:
+        _expect("positions", positions, (n,), torch.int32)
+    else:
+        _expect("positions", positions, (rope.n_axes, n), torch.int32)
+    _expect_on(x.device, out=out, positions=positions)
+    _check("pbb_rotate", load_library().pbb_rotate(
+        ctypes.byref(rope), n, heads, _ptr(positions), _ptr(x), xs, _ptr(out), os_, int(inverse), code,
+        _stream(stream)))
+    return out
+
+
+def make_paged_desc(batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, *, page_size: int,
+                    n_pages: int, table_width: int, block: int = 0, window: int = 0,
+                    dtype=torch.bfloat16, scale: float = 0.0) -> PbbPagedDesc:
+    """Descriptor of a paged cache and the layer that attends over it: PBB (``block`` > 0), sliding
+    window (``window`` > 0), or every position up to the token's own (neither)."""
+    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}.get(dtype, dtype)
+    return PbbPagedDesc(batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, table_width, block,
+                        window, int(code), float(scale))
+
+
+def pages_shape(desc: PbbPagedDesc):
+    return (desc.n_pages, desc.n_kv_heads, desc.page_size, desc.head_dim)
+
+
+def alloc_pages(desc: PbbPagedDesc, device="cuda"):
+    """Allocate (uninitialised) K and V pages for ``desc``."""
+    return tuple(torch.empty(pages_shape(desc), dtype=desc.torch_dtype, device=device)
+                 for _ in range(2))
+
+
+def paged_workspace_bytes(desc: PbbPagedDesc, n_tokens: int) -> int:
+    out = ctypes.c_size_t()
+    _check("pbb_paged_workspace_bytes", load_library().pbb_paged_workspace_bytes(
+        ctypes.byref(desc), int(n_tokens), ctypes.byref(out)))
+    return out.value
+
+
+PAGED_COUNTER_BYTES = 16384
+
+
+def alloc_paged_workspace(desc: PbbPagedDesc, n_tokens: int, device="cuda"):
+    """Workspace for :func:`pbb_paged_attention` calls of up to ``n_tokens`` tokens, its counters
+    zero, or None when they need none.  Calls leave the counters zero, so one allocation serves every
+    later call on one stream (calls that may overlap need their own)."""
+    n = paged_workspace_bytes(desc, n_tokens)
+    if n == 0:
+        return None
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:PAGED_COUNTER_BYTES].zero_()
+    return ws
+
+
+def _expect_paged(desc: PbbPagedDesc, n: int, pos, table, q_start, k_pages, v_pages):
+    _expect("pos", pos, (desc.batch,), torch.int32)
+    _expect("table", table, (desc.batch, desc.table_width), torch.int32)
+    if q_start is not None:
+        _expect("q_start", q_start, (desc.batch + 1,), torch.int32)
+    shape, dtype = pages_shape(desc), desc.torch_dtype
+    _expect("k_pages", k_pages, shape, dtype)
+    _expect("v_pages", v_pages, shape, dtype)
+
+
+def pbb_paged_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, q_start=None, rope=None,
+                     rope_pos=None, q=None, q_out=None, stream=None):
+    """Append the new tokens of every sequence to the cache (see ``include/pbb.h``): ``k``, ``v``
+    [tokens][Hkv][d] packed by ``q_start`` (None: the same number for every sequence), ``rope``
+    applied to ``k`` and, into ``q_out``, to ``q`` [tokens][Hq][d]."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k: must be [tokens][Hkv][d]")
+    n, dtype = k.shape[0], desc.torch_dtype
+    _expect_paged(desc, n, pos, table, q_start, k_pages, v_pages)
+    kv = (n, desc.n_kv_heads, desc.head_dim)
+    ks, vs, qs = _expect_rows("k", k, kv, dtype), _expect_rows("v", v, kv, dtype), 0
+    if (q is None) != (q_out is None):
+        raise ValueError("pbb_paged_append: pass both q and q_out or neither")
+    if q is not None:
+        heads = (n, desc.n_q_heads, desc.head_dim)
+        qs = _expect_rows("q", q, heads, dtype)
+        _expect("q_out", q_out, heads, dtype)
+    if rope_pos is not None:
+        if rope is None:
+            raise ValueError("pbb_paged_append: rope_pos without rope")
+        _expect("rope_pos", rope_pos, (rope.n_axes, n), torch.int32)
+    _expect_on(k.device, pos=pos, table=table, q_start=q_start, k_pages=k_pages, v_pages=v_pages, v=v,
+               q=q, q_out=q_out, rope_pos=rope_pos)
+    _check("pbb_paged_append", load_library().pbb_paged_append(
+        ctypes.byref(desc), n, _ptr(pos), _ptr(q_start), _ptr(table),
+        None if rope is None else ctypes.byref(rope), _ptr(rope_pos), _ptr(q), qs, _ptr(q_out),
+        _ptr(k), ks, _ptr(v), vs, _ptr(k_pages), _ptr(v_pages), _stream(stream)))
+
+
+def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out, q_start=None,
+                        lse=None, workspace=None, stream=None):
+    """Attention of the new tokens over the cache that holds them (see ``include/pbb.h``): ``q``,
+    ``out`` [tokens][Hq][d] packed by ``q_start``; optional ``lse`` [Hq][tokens] (float32).
+    Allocates the workspace when none is given."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q: must be [tokens][Hq][d]")
+    n, dtype = q.shape[0], desc.torch_dtype
+    _expect_paged(desc, n, pos, table, q_start, k_pages, v_pages)
+    heads = (n, desc.n_q_heads, desc.head_dim)
+    qs = _expect_rows("q", q, heads, dtype)
+    _expect("out", out, heads, dtype)
+    if lse is not None:
+        _expect("lse", lse, (desc.n_q_heads, n), torch.float32)
+    _expect_on(q.device, pos=pos, table=table, q_start=q_start, k_pages=k_pages, v_pages=v_pages,
+               out=out, lse=lse, workspace=workspace)
+    if workspace is None and paged_workspace_bytes(desc, n) > 0:
+        workspace = _scratch_on(stream, lambda: alloc_paged_workspace(desc, n, q.device))
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check("pbb_paged_attention", load_library().pbb_paged_attention(
+        ctypes.byref(desc), n, _ptr(pos), _ptr(q_start), _ptr(table), _ptr(q), qs, _ptr(k_pages),
+        _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)))
+    return out
