@@ -14,8 +14,11 @@
 //
 // Masks.  Steps with a key outside some column's support set its scores to -inf.  What such keys hold
 // is unknown (rows never written, dropped pages), and 0 * inf or 0 * NaN would reach the products, so
-// masked steps look whether any value that they read is infinite or NaN, and if so take them apart:
-// finite values enter the product, the others only the columns that see their key.
+// masked steps look whether any value that they read is infinite or NaN, and if so clear those; after
+// the walk, a wave that met one adds them to the columns that see their keys (handling them on the
+// spot costs registers that every step needs).
+
+#include <type_traits>
 
 #include "pbb_paged_device.h"
 
@@ -45,19 +48,10 @@ __device__ __forceinline__ bool any_special(const u32x2 (&v)[N]) {
   return top[0] >= 0x7F80 || top[1] >= 0x7F80;
 }
 
-// A word of two bf16 values: finite ones (others 0), and 1.0 for each that is +inf or NaN (SIGN 0),
-// or -inf or NaN (SIGN 1).
+// The halves of a word of two bf16 values that are infinite or NaN.
 __device__ __forceinline__ uint32_t special_halves(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
          ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-}
-template <int SIGN>
-__device__ __forceinline__ uint32_t ones_where(uint32_t w) {
-  auto half = [](uint32_t h) -> uint32_t {
-    const bool special = (h & 0x7F80u) == 0x7F80u, nan = special && (h & 0x7Fu) != 0;
-    return special && (nan || (h >> 15) == (uint32_t)SIGN) ? 0x3F80u : 0u;
-  };
-  return half(w & 0xFFFFu) | (half(w >> 16) << 16);
 }
 
 template <int D, int ST, int OCC>
@@ -153,29 +147,35 @@ void paged_bf16_kernel(PagedArgs a) {
   // bits per step, the youngest lowest).
   const unsigned char* const pool = (const unsigned char*)(wave >= 2 ? a.v_pages : a.k_pages);
   const int32_t* const table = a.table + (size_t)it.b * sh.width;
+  const uint32_t page_bytes = (uint32_t)sh.page_size * ROWB;   // of one KV head
+  const uint64_t page_stride = (uint64_t)page_bytes * (uint32_t)a.hkv;
+  const unsigned char* const heads = pool + (uint64_t)page_bytes * (uint32_t)g;
   int next_key = s_first * 32;   // first key of the step to be issued next
   int id0 = 0, id1 = 0;          // its entries (the two halves')
+  bool past = false;             // the second half lies past the table
+  uint32_t slot_b = 0;           // bytes from its page to this wave's half
   auto fetch = [&]() {
     const int i0 = sh.by_page.div(next_key), i1 = sh.by_page.div(next_key + 16);
-    id0 = i0 < sh.width ? scalar_word(table, i0) : -1;
-    id1 = i1 < sh.width ? scalar_word(table, i1) : -1;
+    id0 = scalar_word(table, min(i0, sh.width - 1));
+    id1 = scalar_word(table, min(i1, sh.width - 1));
+    past = i1 >= sh.width;
+    const int i = (wave & 1) ? i1 : i0;
+    slot_b = (uint32_t)(next_key + 16 * (wave & 1) - i * sh.page_size) * ROWB;
   };
   uint32_t gone = 0;
   uint32_t doff[kDmaBlocks<D>];
   dma_offsets<D>(lane, ROWB, doff);
   auto issue = [&](int stage) {   // the next step
-    gone |= (sh.is_page(id0) ? 0u : 1u) | (sh.is_page(id1) ? 0u : 2u);
-    const int key = next_key + 16 * (wave & 1);
-    const int id = (wave & 1) ? id1 : id0;
-    const int slot = key - sh.by_page.div(key) * sh.page_size;
-    const unsigned char* src =
-        pool + (((size_t)(sh.is_page(id) ? id : 0) * a.hkv + g) * sh.page_size + slot) * ROWB;
+    const bool ok0 = sh.is_page(id0), ok1 = sh.is_page(id1) && !past;
+    gone |= (ok0 ? 0u : 1u) | (ok1 ? 0u : 2u);
+    const uint32_t id0s = ok0 ? (uint32_t)id0 : 0u, id1s = ok1 ? (uint32_t)id1 : 0u;
+    const uint32_t id = (wave & 1) ? id1s : id0s;
+    const unsigned char* src = heads + id * page_stride + slot_b;
     unsigned char* lds = smem + stage * BUF + wave * HALF;
 #pragma unroll
     for (int y = 0; y < 2 * kDmaBlocks<D>; ++y)
       dma16(y < kDmaBlocks<D> ? src : src + 8 * ROWB, doff[y % kDmaBlocks<D>], lds + 1024 * y);
     next_key += 32;
-    fetch();
   };
   fetch();
 
@@ -184,6 +184,7 @@ void paged_bf16_kernel(PagedArgs a) {
   for (int s = 0; s < STAGES - 1; ++s) {
     gone <<= 2;
     if (s < nsteps) issue(s);
+    fetch();
   }
 
   // LDS byte addresses of this lane's reads in stage 0 (tile_addresses; the V tile is TILE on).
@@ -222,6 +223,7 @@ void paged_bf16_kernel(PagedArgs a) {
   }
   const float sc = a.scale_log2;
 
+  bool odd = false;   // a masked step held an infinity or NaN
   int rstage = 0;
   constexpr int OPS = D / 32;           // DMA instructions of a wave per step
 
@@ -240,7 +242,7 @@ void paged_bf16_kernel(PagedArgs a) {
     return sb;
   };
 
-  auto step = [&](int st, uint32_t sb) {
+  auto step = [&](int st, uint32_t sb, uint32_t dropped, bool masked) {
     f32x4 s0[QC], s1[QC];
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
@@ -258,9 +260,11 @@ void paged_bf16_kernel(PagedArgs a) {
         s1[qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qB[qc][kk], s1[qc], 0, 0, 0);
       }
     }
+    // The next step's entries, here so that no wait for LDS reads waits for them too.
+    __builtin_amdgcn_sched_barrier(0);
+    fetch();
+    __builtin_amdgcn_sched_barrier(0);
     // Element e of s0 is key k0 + 4 j4 + e of the lane's column, of s1 key k0 + 16 + 4 j4 + e.
-    const uint32_t dropped = (gone >> (2 * (STAGES - 1))) & 3u;
-    const bool masked = st < ua || st >= ub || dropped != 0;
     const int k0 = (s_first + st) * 32 + 4 * j4;
     auto seen = [&](int qc, int e) -> bool {   // element e: 0..3 of s0, 4..7 of s1
       const int k = e < 4 ? e : e + 12;
@@ -333,37 +337,11 @@ void paged_bf16_kernel(PagedArgs a) {
     read_chunks<D, TILE>(vr, va, sb);
     wait_chunks<D>(vr);
     if (masked && __builtin_amdgcn_ballot_w64(any_special(vr)) != 0) {
-      // Infinities and NaN among the step's values: 1 for each that is +inf or NaN (-inf or NaN),
-      // times 1 for each key that the column sees, counts those that a column's output takes.
-      bf16x8 one[QC];
+      odd = true;
 #pragma unroll
-      for (int qc = 0; qc < QC; ++qc)
+      for (int i = 0; i < 2 * NB; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) one[qc][e] = seen(qc, e) ? (__bf16)1.0f : (__bf16)0.0f;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        u32x2 up[2], down[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t w = vr[2 * nb + i][e];
-            up[i][e] = ones_where<0>(w);
-            down[i][e] = ones_where<1>(w);
-            vr[2 * nb + i][e] = w & ~special_halves(w);
-          }
-#pragma unroll
-        for (int qc = 0; qc < QC; ++qc) {
-          const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-          const f32x4 cu = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join_chunks(up[0], up[1]), one[qc],
-                                                                   z, 0, 0, 0);
-          const f32x4 cd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join_chunks(down[0], down[1]),
-                                                                   one[qc], z, 0, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[qc][nb][e] += (cu[e] > 0.0f ? -kNegInf : 0.0f) + (cd[e] > 0.0f ? kNegInf : 0.0f);
-        }
-      }
+        for (int e = 0; e < 2; ++e) vr[i][e] &= ~special_halves(vr[i][e]);
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -376,12 +354,45 @@ void paged_bf16_kernel(PagedArgs a) {
   };
 
   int st = 0;
-  for (; st < wlo && st < nsteps; ++st) begin_step(st);
+  for (; st < wlo && st < nsteps; ++st) begin_step(st), fetch();
   for (; st <= whi; ++st) {
     const uint32_t sb = begin_step(st);
-    step(st, sb);
+    const uint32_t dropped = (gone >> (2 * (STAGES - 1))) & 3u;
+    step(st, sb, dropped, st < ua || st >= ub || dropped != 0);
   }
-  for (; st < nsteps; ++st) begin_step(st);
+  for (; st < nsteps; ++st) begin_step(st), fetch();
+
+  if (odd) {
+    // The infinities and NaN of masked steps, straight from the pages: their weights are positive,
+    // so each enters the columns that see its key as it is.
+    const unsigned char* const values = (const unsigned char*)a.v_pages + (uint64_t)page_bytes * (uint32_t)g;
+    for (st = wlo; st <= whi; ++st) {
+      const int first = (s_first + st) * 32;
+      const int e0 = sh.by_page.div(first), e1 = sh.by_page.div(first + 16);
+      const bool whole = e1 < sh.width && sh.is_page(scalar_word(table, e0)) &&
+                         sh.is_page(scalar_word(table, min(e1, sh.width - 1)));
+      if (st >= ua && st < ub && whole) continue;
+      for (int key = first; key < first + 32; ++key) {
+        const int i = sh.by_page.div(key);
+        const int id = i < sh.width ? scalar_word(table, min(i, sh.width - 1)) : -1;
+        if (!sh.is_page(id)) continue;
+        const unsigned char* row = values + (uint32_t)id * page_stride +
+                                   (uint32_t)(key - i * sh.page_size) * ROWB + 8 * j4;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const u32x2 w = *(const u32x2*)(row + 32 * nb);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t h = e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16;
+            const float add = (h & 0x7F800000u) == 0x7F800000u ? __uint_as_float(h) : 0.0f;
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc)
+              acc[qc][nb][e] += key >= lo_c[qc] && key <= tcol[qc] ? add : 0.0f;
+          }
+        }
+      }
+    }
+  }
 
   // Output of a column: o = acc / l (bf16 RNE), lse = (m + log2 l) * ln 2; an empty support has l 0
   // and gets zeros and -inf.
