@@ -369,7 +369,7 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t *desc, int32_t n_tokens, co
  * call on one stream, for any descriptor it is large enough for; calls that may run concurrently
  * (captured graphs among them) need separate workspaces.
  */
-#define PBB_PAGED_COUNTER_BYTES 16384u
+#define PBB_PAGED_COUNTER_BYTES 65536u
 pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_tokens,
                                        size_t *bytes);
 

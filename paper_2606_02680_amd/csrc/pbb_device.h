@@ -261,6 +261,26 @@ __device__ __forceinline__ void read_chunks(u32x2 (&dst)[D / 8], const uint32_t 
   }
 }
 
+// The same of a 16-row tile: dst[nb] holds rows 4j4 .. +3 of channel 16nb + c16.
+template <int D>
+__device__ __forceinline__ void read_tile(u32x2 (&dst)[D / 16], const uint32_t (&ta)[4], uint32_t sb) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) dst[x] = tr_read<0>(ta[x] + sb);
+  if constexpr (D == 128) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) dst[4 + x] = tr_read<kTileLine>(ta[x] + sb);
+  }
+}
+template <int D>
+__device__ __forceinline__ void wait_tile(u32x2 (&v)[D / 16]) {
+  if constexpr (D == 128)
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]),
+                   "+v"(v[6]), "+v"(v[7]));
+  else
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+}
+
 __device__ __forceinline__ bf16x8 join_chunks(u32x2 x, u32x2 y) {
   const u32x4 w = {x[0], x[1], y[0], y[1]};
   return __builtin_bit_cast(bf16x8, w);

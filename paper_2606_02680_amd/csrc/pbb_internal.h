@@ -177,11 +177,19 @@ struct PagedArgs {
   PagedPlan plan;
 };
 
-// Query columns (tokens of a tile times the heads of a group) and keys per step of the paged
-// attention kernels.
+// Kinds of paged attention kernels.
 constexpr int kPagedCols = 128, kPagedStep = 32;          // bf16
 constexpr int kPagedColsF32 = 64, kPagedStepF32 = 16;     // fp32
-constexpr size_t kPagedCounterBytes = 16384;
+inline PagedKind paged_kind(bool f32, bool narrow, int head_dim) {
+  if (f32) return PagedKind{narrow ? kPagedNarrowCols : kPagedColsF32, kPagedStepF32, 768, 8, 1024, 32};
+  // Single tokens: one workgroup per CU where there are few (d = 128; 32/8 heads, one sequence of
+  // 32000 28.2 us, against 32.4 and 36.7 for two and three per CU; eight of up to 8000 30.3 / 31.2 /
+  // 32.9).  Many: pieces of fewer than 64 steps cost more than an even end gains (256 sequences of
+  // up to 600: 73 us, 115 with pieces of 8); 2048 of them, not 1024 (192 of up to 32768: 1870 / 1934).
+  if (narrow) return PagedKind{kPagedNarrowCols, kPagedStep, head_dim == 64 ? 512 : 256, 8, 2048, 64};
+  return PagedKind{kPagedCols, kPagedStep, 0, 32, 1024, 32};
+}
+constexpr size_t kPagedCounterBytes = 65536;
 
 // Bytes of one partial state: an unnormalised output, a reference and a sum per column.
 constexpr size_t paged_state_bytes(int cols, int head_dim) {

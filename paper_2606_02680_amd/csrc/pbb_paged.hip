@@ -35,6 +35,7 @@ constexpr int kPagedStages64 = 4, kPagedOcc64 = 4;
 constexpr float kNoScore = -3.0e38f;
 
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 // Whether one of the bf16 values of an operand is infinite or NaN.
 template <int N>
@@ -54,6 +55,308 @@ __device__ __forceinline__ uint32_t special_halves(uint32_t w) {
          ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
 
+// Few columns: tiles of at most 16 (single tokens, short drafts).  The 16-key halves of the piece's
+// steps are dealt to the waves one by one, each with LDS tiles of its own, so that nothing but the
+// merge of the waves at the end waits for another wave.  A wave has three 16-row tiles: while it works
+// on one, the two after it (K and V rows alternate) are in flight; a tile is loaded over as soon as it
+// has been read.  The value products contract 16 keys (v_mfma_f32_16x16x16_bf16).
+// Bound: HBM, with 12 waves per CU, 8 KiB of each in flight.
+template <int D>
+constexpr int narrow_lds() { return kPagedWaves * 3 * 16 * D * 2; }
+
+template <int D, bool IN_PLACE>
+__device__ __forceinline__ void narrow_walk(const PagedArgs& a, const PagedItem& it, int g,
+                                            unsigned char* smem) {
+  constexpr int NW = kPagedWaves;
+  constexpr int KK = D / 32;
+  constexpr int NB = D / 16;
+  constexpr int ROWB = D * 2;
+  constexpr int TILE = 16 * ROWB;       // 16 rows of K or V
+  constexpr int OPS = TILE / 1024;      // DMA instructions of a tile
+  constexpr int COLS = kPagedNarrowCols;
+  constexpr int MERGE = NW * COLS * (D + 2) * 4;
+  static_assert(MERGE + 16 <= narrow_lds<D>(), "the merge of the waves fits their tiles");
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15;
+  const int j4 = lane >> 4;
+  const int G = a.group;
+  const PagedPlan& pl = a.plan;
+  const PagedShape& sh = a.shape;
+  const int tokens = it.c.count;
+  const int64_t row0 = it.c.row0;
+  const int cols = tokens * G;
+  auto address = [&](int col) -> int64_t {   // output row of a column
+    const int cp = pl.by_group.div(col);
+    return (row0 + cp) * a.hq + (int64_t)(g * G + col - cp * G);
+  };
+  auto lse_at = [&](int col) -> int64_t {
+    const int cp = pl.by_group.div(col);
+    return (int64_t)(g * G + col - cp * G) * a.n + row0 + cp;
+  };
+  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
+    if (it.piece > 0) return;
+    for (int i = tid; i < cols * (ROWB / 16); i += NW * 64) {
+      const int col = i / (ROWB / 16);
+      *(u32x4*)((unsigned char*)a.out + address(col) * ROWB + (i - col * (ROWB / 16)) * 16) =
+          u32x4{0u, 0u, 0u, 0u};
+    }
+    if (a.lse != nullptr && tid < cols) a.lse[lse_at(tid)] = kNegInf;
+    return;
+  }
+
+  // Halves [h0, h1) of the piece (half h: keys 16 h .. 16 h + 15).
+  const int t0 = it.c.pos;
+  const int t_last = t0 + tokens - 1;
+  const int s_first = sh.support_lo(t0) >> 5;
+  const int last_key = min(t_last, sh.capacity - 1);
+  const int nsteps = max(0, (last_key >> 5) - s_first + 1);
+  int h0 = 2 * s_first, h1 = min(2 * (s_first + nsteps), (last_key >> 4) + 1);
+  if (it.ways > 1) {
+    h1 = min(h1, 2 * (s_first + (int)((int64_t)(it.piece + 1) * nsteps / it.ways)));
+    h0 = 2 * (s_first + (int)((int64_t)it.piece * nsteps / it.ways));
+  }
+  if (h1 <= h0) h0 = h1 = 0;   // (positions past the table: 16 h would pass 2^31)
+
+  // This lane's column (past the tile's: the last token's row, a zero query, no key seen).
+  const int cp = min(pl.by_group.div(c16), tokens - 1);
+  const bool valid = c16 < cols;
+  const int tcol = valid ? t0 + cp : -1;
+  const int lo_c = sh.support_lo(t0 + cp);
+  bf16x8 qB[KK];
+  {
+    const unsigned char* qrow = (const unsigned char*)a.q + (row0 + cp) * a.q_stride +
+                                (int64_t)(g * G + (valid ? c16 - cp * G : 0)) * ROWB + 16 * j4;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qB[kk] = *(const bf16x8*)(qrow + 64 * kk);
+  }
+
+  // A half's page entry through the scalar cache, a half before its loads.
+  const int32_t* const table = a.table + (size_t)it.b * sh.width;
+  const uint32_t page_bytes = (uint32_t)sh.page_size * ROWB;   // of one KV head
+  const uint64_t page_stride = (uint64_t)page_bytes * (uint32_t)a.hkv;
+  const unsigned char* const keys = (const unsigned char*)a.k_pages + (uint64_t)page_bytes * (uint32_t)g;
+  const unsigned char* const values = (const unsigned char*)a.v_pages + (uint64_t)page_bytes * (uint32_t)g;
+  struct Entry { int id; uint32_t slot; };
+  auto fetch = [&](int h) -> Entry {   // (halves past the walk read the last entry, for nothing)
+    const int i = min(sh.by_page.div(16 * h), sh.width - 1);
+    return Entry{scalar_word(table, i), (uint32_t)(16 * h - i * sh.page_size) * ROWB};
+  };
+  auto offset = [&](const Entry& e) -> uint64_t {
+    return (sh.is_page(e.id) ? (uint32_t)e.id : 0u) * page_stride + e.slot;
+  };
+  uint32_t doff[kDmaBlocks<D>];
+  dma_offsets<D>(lane, ROWB, doff);
+  unsigned char* const wbuf = smem + wave * 3 * TILE;
+  auto load = [&](const unsigned char* src, int tile) {   // (non-temporal: read once in a call)
+#pragma unroll
+    for (int y = 0; y < OPS; ++y)
+      __builtin_amdgcn_global_load_lds(
+          (const void*)((y < kDmaBlocks<D> ? src : src + 8 * ROWB) + doff[y % kDmaBlocks<D>]),
+          (__attribute__((address_space(3))) void*)(wbuf + tile + 1024 * y), 16, 0, kCachePolicyNT);
+  };
+  int h = h0 + wave;
+  bool gone = false, next_gone = false;   // the half's, and the next one's, keys have no page
+  uint64_t next_off = 0;
+  Entry after = {0, 0};
+  if (h < h1) {
+    const Entry e0 = fetch(h), e1 = fetch(min(h + NW, h1 - 1));
+    after = fetch(min(h + 2 * NW, h1 - 1));
+    gone = !sh.is_page(e0.id);
+    next_gone = !sh.is_page(e1.id);
+    next_off = offset(e1);
+    load(keys + offset(e0), 0);
+    load(values + offset(e0), TILE);
+    if (h + NW < h1) load(keys + next_off, 2 * TILE);
+  }
+
+  uint32_t ra[2], va[4];
+  {
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)wbuf;
+    tile_addresses<D>(base, c16, j4, ra, va);
+  }
+  const __attribute__((address_space(3))) unsigned char* lds0 = nullptr;
+  // the run [ua, ub) of halves whose keys all lie in every column's support
+  const int ua = (sh.support_lo(t_last) + 15) >> 4;
+  const int ub = (t0 + 1) >> 4;
+
+  float m = valid ? kNoScore : 0.0f, lsum = 0.0f;
+  f32x4 acc[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) acc[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+    qB[kk] = __builtin_bit_cast(bf16x8, valid ? __builtin_bit_cast(u32x4, qB[kk]) : u32x4{0u, 0u, 0u, 0u});
+  const float sc = a.scale_log2;
+  bool odd = false;
+
+  int kt = 0, vt = TILE, nt = 2 * TILE;   // tiles of this half's keys and values, of the next one's keys
+  for (; h < h1; h += NW) {
+    const int more = h + NW < h1 ? (h + 2 * NW < h1 ? 2 : 1) : 0;   // halves after this one (2: or more)
+    // its keys have landed: its values and the next half's keys may be outstanding
+    wait_groups<2, OPS>(more > 0 ? 2 : 1);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    bf16x8 ka[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      ka[kk] = *(const __attribute__((address_space(3))) bf16x8*)(lds0 + ra[kk & 1] + kt +
+                                                                   kTileLine * (kk >> 1));
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kk], qB[kk], s, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    // (the keys have been read: the next half's values go over them)
+    if (more > 0) load(values + next_off, kt);
+    const bool masked = h < ua || h >= ub || gone;
+    if (masked) {
+      const int k0 = 16 * h + 4 * j4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s[e] = e >= lo_c - k0 && e <= tcol - k0 && !gone ? s[e] : kNegInf;
+    }
+    float p[4], ps;
+    auto weights = [&]() {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(__builtin_fmaf(s[e], sc, -m));
+      ps = (p[0] + p[1]) + (p[2] + p[3]);
+      return !(ps <= kWeightCap);
+    };
+    auto column_max = [&]() {
+      return max_xor16_32(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * sc;
+    };
+    if (h == h0 + wave) m = fmaxf(m, column_max());
+    if (__builtin_amdgcn_ballot_w64(weights()) != 0) {
+      const float cand = column_max();
+      const bool grow = cand > m && max_xor16_32(ps) > kWeightCap;
+      const float alpha = grow ? fast_exp2(m - cand) : 1.0f;
+      m = grow ? cand : m;
+      lsum *= alpha;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) acc[nb] *= alpha;
+      weights();
+    }
+    lsum += ps;
+    const u32x2 pB = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
+    // its values have landed: the next half's keys and values may be outstanding
+    wait_groups<2, OPS>(more > 0 ? 2 : 0);
+    __builtin_amdgcn_sched_barrier(0);
+    u32x2 vr[NB];
+    read_tile<D>(vr, va, (uint32_t)vt);
+    wait_tile<D>(vr);
+    if (masked && __builtin_amdgcn_ballot_w64(any_special(vr)) != 0) {
+      odd = true;
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) vr[i][e] &= ~special_halves(vr[i][e]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // (the values have been read: the keys of the half after next go over them)
+    gone = next_gone;
+    next_gone = !sh.is_page(after.id);
+    next_off = offset(after);
+    if (more > 1) load(keys + next_off, vt);
+    after = fetch(min(h + 3 * NW, h1 - 1));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      acc[nb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+          __builtin_bit_cast(s16x4, vr[nb]), __builtin_bit_cast(s16x4, pB), acc[nb], 0, 0, 0);
+    const int t = kt;
+    kt = nt;
+    nt = vt;
+    vt = t;
+  }
+  if (odd) {   // (see paged_bf16_kernel)
+    for (h = h0 + wave; h < h1; h += NW) {
+      const Entry e = fetch(h);
+      if (!sh.is_page(e.id) || (h >= ua && h < ub)) continue;
+      const unsigned char* row = values + offset(e) + 8 * j4;
+      for (int key = 16 * h; key < 16 * h + 16; ++key, row += ROWB) {
+        const bool sees = key >= lo_c && key <= tcol;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const u32x2 w = *(const u32x2*)(row + 32 * nb);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16;
+            acc[nb][e] += sees && (x & 0x7F800000u) == 0x7F800000u ? __uint_as_float(x) : 0.0f;
+          }
+        }
+      }
+    }
+  }
+
+  // The waves' states through LDS (Eq.(lse)); each thread takes 4 channels of a column.
+  lsum = sum_xor16_32(lsum);
+  __syncthreads();   // every wave is done with its tiles
+  float* const sm_acc = (float*)smem;               // [NW][COLS][D]
+  float* const sm_m = sm_acc + NW * COLS * D;       // [NW][COLS]
+  float* const sm_l = sm_m + NW * COLS;
+  int* const last_one = (int*)(smem + MERGE);
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+    *(f32x4*)(sm_acc + (wave * COLS + c16) * D + 16 * nb + 4 * j4) = acc[nb];
+  if (j4 == 0) {
+    sm_m[wave * COLS + c16] = m;
+    sm_l[wave * COLS + c16] = lsum;
+  }
+  __syncthreads();
+  constexpr int SCOLS = IN_PLACE ? COLS : kPagedCols;
+  constexpr size_t STATE = paged_state_bytes(SCOLS, D) / 4;
+  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
+  float* const part = a.states + (unit + it.piece) * STATE;
+  for (int i = tid; i < cols * (D / 4); i += NW * 64) {
+    const int col = i / (D / 4), q = i - col * (D / 4);
+    float M = kNoScore;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * COLS + col]);
+    float L = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {   // (a wave that saw nothing holds zeros)
+      const float wt = fast_exp2(sm_m[w * COLS + col] - M);
+      L += wt * sm_l[w * COLS + col];
+      o += wt * *(const f32x4*)(sm_acc + (w * COLS + col) * D + 4 * q);
+    }
+    if (it.ways == 1) {
+      store4((uint16_t*)a.out + address(col) * D + 4 * q, o, inverse_sum(L));
+      if (a.lse != nullptr && q == 0) a.lse[lse_at(col)] = log_partition(M, L);
+    } else if (IN_PLACE) {
+      coherent_store2(part + col * D + 4 * q, o[0], o[1]);
+      coherent_store2(part + col * D + 4 * q + 2, o[2], o[3]);
+      if (q == 0) coherent_store2(part + SCOLS * D + 2 * col, M, L);
+    } else {
+      *(f32x4*)(part + col * D + 4 * q) = o;
+      if (q == 0) *(float2*)(part + SCOLS * D + 2 * col) = make_float2(M, L);
+    }
+  }
+  if (!IN_PLACE || it.ways == 1) return;
+  // A cut walk: the count of its pieces; whoever completes it merges them (coherent_store2 says why
+  // this orders).
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+    *last_one = before == (unsigned)(it.ways - 1);
+    if (*last_one)
+      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!*last_one) return;
+  merge_states<D, SCOLS, NW * 64>(
+      a.states + unit * STATE, STATE, it.ways, cols, tid,
+      [&](int col, int c, f32x4 o, float l) {
+        store4((uint16_t*)a.out + address(col) * D + c, o, inverse_sum(l));
+      },
+      [&](int col, float mref, float l) {
+        if (a.lse != nullptr) a.lse[lse_at(col)] = log_partition(mref, l);
+      });
+}
+
 template <int D, int ST, int OCC>
 __global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_eu(OCC)))
 void paged_bf16_kernel(PagedArgs a) {
@@ -69,7 +372,6 @@ void paged_bf16_kernel(PagedArgs a) {
   static_assert(STAGES >= 3, "stages");
   static_assert(NW == 4, "one (tensor, 16-row half) of a step per wave");
   __shared__ __align__(1024) unsigned char smem[STAGES * BUF];
-  __shared__ int last_one;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -83,7 +385,12 @@ void paged_bf16_kernel(PagedArgs a) {
   const int item = pl.by_hkv.div((int)blockIdx.x);
   const int g = (int)blockIdx.x - item * a.hkv;
   PagedItem it;
-  if (!find_item(a, item, lane, it)) return;
+  if (!find_item<false>(a, item, lane, it)) return;
+  if (it.c.count * G <= kPagedNarrowCols) {
+    static_assert(narrow_lds<D>() <= STAGES * BUF, "LDS");
+    narrow_walk<D, false>(a, it, g, smem);
+    return;
+  }
   const int p0 = it.tile * pl.tq;                               // the tile's tokens in the chunk
   const int tokens = min(pl.tq, it.c.count - p0);
   const int64_t row0 = (int64_t)it.c.row0 + p0;                 // packed row of the first one
@@ -109,6 +416,7 @@ void paged_bf16_kernel(PagedArgs a) {
   const int t_last = t0 + tokens - 1;
   int s_first = sh.support_lo(t0) >> 5;
   int nsteps = max(0, (min(t_last, sh.capacity - 1) >> 5) - s_first + 1);
+  if (nsteps == 0) s_first = 0;   // (all past the table: positions whose next steps pass 2^31)
   if (it.ways > 1) {
     const int lo = (int)((int64_t)it.piece * nsteps / it.ways);
     const int hi = (int)((int64_t)(it.piece + 1) * nsteps / it.ways);
@@ -396,15 +704,11 @@ void paged_bf16_kernel(PagedArgs a) {
 
   // Output of a column: o = acc / l (bf16 RNE), lse = (m + log2 l) * ln 2; an empty support has l 0
   // and gets zeros and -inf.
-  auto inverse = [](float l) { return l == 0.0f ? 0.0f : 1.0f / l; };
-  auto log_partition = [](float mref, float l) {
-    return l == 0.0f ? kNegInf : (mref + __builtin_log2f(l)) * 0.69314718055994531f;
-  };
   if (it.ways == 1) {
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
       const float l = sum_xor16_32(lsum[qc]);
-      const float inv = inverse(l);
+      const float inv = inverse_sum(l);
       u32x4 w[NB / 2];
 #pragma unroll
       for (int q = 0; q < NB / 2; ++q) w[q] = pair_blocks(acc[qc][2 * q], acc[qc][2 * q + 1], inv);
@@ -422,64 +726,59 @@ void paged_bf16_kernel(PagedArgs a) {
     return;
   }
 
-  // A cut walk: the piece's state, device-coherent, then the count of the tile's pieces; whoever
-  // completes it merges them (coherent_store2 says why this orders).
+  // A cut walk leaves the piece's state for the merge launch; the tile's states lie together.
   constexpr size_t STATE = paged_state_bytes(kPagedCols, D) / 4;
-  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
-  float* const part = a.states + (unit + it.piece) * STATE;
+  float* const part =
+      a.states + ((size_t)it.slot * a.hkv + (size_t)g * it.ways + it.piece) * STATE;
 #pragma unroll
   for (int qc = 0; qc < QC; ++qc) {
     const float l = sum_xor16_32(lsum[qc]);
     const int col = (wave * QC + qc) * 16 + c16;
     if (col < cols) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        coherent_store2(part + col * D + 16 * nb + 4 * j4, acc[qc][nb][0], acc[qc][nb][1]);
-        coherent_store2(part + col * D + 16 * nb + 4 * j4 + 2, acc[qc][nb][2], acc[qc][nb][3]);
-      }
-      if (j4 == 0) coherent_store2(part + kPagedCols * D + 2 * col, m[qc], l);
+      for (int nb = 0; nb < NB; ++nb) *(f32x4*)(part + col * D + 16 * nb + 4 * j4) = acc[qc][nb];
+      if (j4 == 0) *(float2*)(part + kPagedCols * D + 2 * col) = make_float2(m[qc], l);
     }
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
-  __syncthreads();
-  if (tid == 0) {
-    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-    last_one = before == (unsigned)(it.ways - 1);
-    if (last_one)
-      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Calls of at most 16 columns per sequence (single tokens, short drafts), and all that they need: the
+// last piece of a cut walk to end merges them.
+template <int D>
+__global__ __launch_bounds__(kPagedWaves * 64) __attribute__((amdgpu_waves_per_eu(3)))
+void paged_narrow_kernel(PagedArgs a) {
+  __shared__ __align__(1024) unsigned char smem[narrow_lds<D>()];
+  const int lane = threadIdx.x & 63;
+  const int item = a.plan.by_hkv.div((int)blockIdx.x);
+  const int g = (int)blockIdx.x - item * a.hkv;
+  PagedItem it;
+  if (!find_item<false>(a, item, lane, it)) return;
+  narrow_walk<D, true>(a, it, g, smem);
+}
+
+}  // namespace
+
+namespace {
+
+template <int D, int ST, int OCC>
+hipError_t launch_paged_t(const PagedArgs& a, hipStream_t stream) {
+  if (a.plan.narrow) {
+    hipLaunchKernelGGL((paged_narrow_kernel<D>), dim3((unsigned)(a.plan.items() * a.hkv)),
+                       dim3(kPagedWaves * 64), 0, stream, a);
+    return hipGetLastError();
   }
-  __syncthreads();
-  if (!last_one) return;
-  auto address = [&](int col) -> int64_t {
-    const int cp = pl.by_group.div(col);
-    return (row0 + cp) * a.hq + (int64_t)(g * G + col - cp * G);
-  };
-  merge_states<D, kPagedCols, NW * 64>(
-      a.states + unit * STATE, STATE, it.ways, cols, tid,
-      [&](int col, int c, f32x4 o, float l) {
-        const float inv = inverse(l);
-        *(u32x2*)((unsigned char*)a.out + address(col) * ROWB + 2 * c) =
-            u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
-      },
-      [&](int col, float mref, float l) {
-        if (a.lse == nullptr) return;
-        const int cp = pl.by_group.div(col);
-        a.lse[(int64_t)(g * G + col - cp * G) * a.n + row0 + cp] = log_partition(mref, l);
-      });
+  hipLaunchKernelGGL((paged_bf16_kernel<D, ST, OCC>), dim3((unsigned)(a.plan.items() * a.hkv)),
+                     dim3(kPagedWaves * 64), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.plan.pieces == 0) return e;
+  return launch_paged_merge<uint16_t, D, kPagedCols>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_paged_bf16(const PagedArgs& a, int32_t head_dim, hipStream_t stream) {
-  const unsigned blocks = (unsigned)(a.plan.items() * a.hkv);
-  if (head_dim == 64)
-    hipLaunchKernelGGL((paged_bf16_kernel<64, kPagedStages64, kPagedOcc64>), dim3(blocks),
-                       dim3(kPagedWaves * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((paged_bf16_kernel<128, kPagedStages128, kPagedOcc128>), dim3(blocks),
-                       dim3(kPagedWaves * 64), 0, stream, a);
-  return hipGetLastError();
+  return head_dim == 64 ? launch_paged_t<64, kPagedStages64, kPagedOcc64>(a, stream)
+                        : launch_paged_t<128, kPagedStages128, kPagedOcc128>(a, stream);
 }
 
 }  // namespace pbb

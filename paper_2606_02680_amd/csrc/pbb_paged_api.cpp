@@ -14,9 +14,9 @@
 namespace {
 
 static_assert(PBB_PAGED_COUNTER_BYTES == pbb::kPagedCounterBytes, "counter block");
-static_assert((2 * pbb::kPagedPieces + pbb::kPagedPieces / 8 + pbb::kPagedPieces) * 4 <=
+static_assert((2 * pbb::kPagedMaxPieces + pbb::kPagedMaxPieces / 8 + pbb::kPagedMaxPieces) * 4 <=
                   (int)pbb::kPagedCounterBytes,
-              "a counter per partial state (2 more per head, of at most kPagedPieces / 2 heads)");
+              "a counter per partial state (2 more per head, of at most kPagedMaxPieces / 2 heads)");
 
 constexpr int32_t kMaxTokens = 1 << 30;
 constexpr int32_t kMaxCapacity = 1 << 30;
@@ -76,17 +76,24 @@ pbb::PagedShape shape_of(const pbb_paged_desc_t* d) {
 }
 
 pbb::PagedPlan plan_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s, int32_t n, bool ragged) {
-  const bool f32 = d->dtype == PBB_DTYPE_F32;
-  return pbb::PagedPlan::make(s, d->batch, d->n_kv_heads, d->n_q_heads / d->n_kv_heads, n, ragged,
-                              f32 ? pbb::kPagedColsF32 : pbb::kPagedCols,
-                              f32 ? pbb::kPagedStepF32 : pbb::kPagedStep);
+  const int group = d->n_q_heads / d->n_kv_heads;
+  const bool narrow = pbb::PagedPlan::is_narrow(d->batch, group, n, ragged);
+  return pbb::PagedPlan::make(s, pbb::paged_kind(d->dtype == PBB_DTYPE_F32, narrow, d->head_dim),
+                              d->batch, d->n_kv_heads, group, n, ragged);
 }
 
-size_t workspace_of(const pbb_paged_desc_t* d, const pbb::PagedPlan& p) {
-  if (p.slots == 0) return 0;
-  const int cols = d->dtype == PBB_DTYPE_F32 ? pbb::kPagedColsF32 : pbb::kPagedCols;
-  return pbb::kPagedCounterBytes +
-         (size_t)p.slots * d->n_kv_heads * pbb::paged_state_bytes(cols, d->head_dim);
+// What any call may need, of few columns per sequence or of many (which of them a call is, its
+// q_start decides).
+size_t workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
+  const int group = d->n_q_heads / d->n_kv_heads;
+  size_t bytes = 0;
+  for (const bool narrow : {false, true}) {
+    const pbb::PagedKind k = pbb::paged_kind(d->dtype == PBB_DTYPE_F32, narrow, d->head_dim);
+    const size_t need = (size_t)pbb::PagedPlan::max_slots(s, k, d->n_kv_heads, k.cols / group) *
+                        d->n_kv_heads * pbb::paged_state_bytes(k.cols, d->head_dim);
+    bytes = need > bytes ? need : bytes;
+  }
+  return bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;
 }
 
 }  // namespace
@@ -207,7 +214,7 @@ pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t* desc, int32_t n_t
   if (desc == nullptr || bytes == nullptr) return PBB_ERR_NULL;
   const pbb_status_t st = check_paged(desc, n_tokens);
   if (st != PBB_OK) return st;
-  *bytes = workspace_of(desc, plan_of(desc, shape_of(desc), n_tokens, true));
+  *bytes = workspace_of(desc, shape_of(desc));
   return PBB_OK;
 }
 
@@ -230,7 +237,7 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   pbb::PagedArgs a;
   a.shape = shape_of(desc);
   a.plan = plan_of(desc, a.shape, n_tokens, q_start != nullptr);
-  const size_t need = workspace_of(desc, a.plan);
+  const size_t need = workspace_of(desc, a.shape);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
   if ((uint64_t)a.plan.items() * (uint64_t)desc->n_kv_heads > 0x7fffffffull) return PBB_ERR_SHAPE;

@@ -2,6 +2,8 @@
 // addresses, and the merge of cut walks.
 #pragma once
 
+#include <type_traits>
+
 #include "pbb_device.h"
 #include "pbb_internal.h"
 
@@ -49,7 +51,9 @@ struct PagedItem {
 // Item `item` of a KV head (false: there are not that many).  Every wave finds it by itself, 64
 // sequences at a time: their counts of pieces, and a sum over the lanes.  Items go sequence by
 // sequence; of one sequence, piece by piece from the last tile (the longest walk) to the first, so
-// that workgroups running side by side read the same keys.
+// that workgroups running side by side read the same keys.  CUT: the items are the tiles whose walks
+// are cut (piece 0).
+template <bool CUT>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane, PagedItem& it) {
   const PagedPlan& p = a.plan;
   auto chunk = [&](int b) -> Chunk {
@@ -58,49 +62,67 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     return chunk_of(b, p.uniform, ragged ? a.q_start[b] : 0, ragged ? a.q_start[b + 1] : 0, a.pos[b],
                     a.n);
   };
-  const Chunk c0 = chunk(lane);
+  // the first 256 sequences' chunks, their loads in flight together
+  constexpr int KEPT = 4;
+  Chunk kept[KEPT];
+#pragma unroll
+  for (int r = 0; r < KEPT; ++r) kept[r] = chunk(64 * r + lane);
+  auto round = [&](auto&& visit) {   // visit(first sequence, this lane's chunk): false ends it
+#pragma unroll
+    for (int r = 0; r < KEPT; ++r) {
+      if (64 * r >= a.batch) return;
+      if (!visit(64 * r, kept[r])) return;
+    }
+    for (int b0 = 64 * KEPT; b0 < a.batch; b0 += 64)
+      if (!visit(b0, chunk(b0 + lane))) return;
+  };
   float share = 1.0e30f;
   if (p.pieces > 0) {
-    float total = 0.0f;
-    uint32_t tiles = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      const Chunk c = b0 == 0 ? c0 : chunk(b0 + lane);
+    float sum = 0.0f;
+    uint32_t count = 0;
+    round([&](int, const Chunk& c) {
       const int nt = p.tiles_of(c);
-      total += __uint_as_float((uint32_t)lane_value(
-          (int)__float_as_uint(wave_scan((float)nt * (float)p.steps_of(a.shape, c))), 63));
-      tiles += (uint32_t)lane_value((int)wave_scan((uint32_t)nt), 63);
-    }
+      sum += (float)nt * (float)p.steps_of(a.shape, c);
+      count += (uint32_t)nt;
+      return true;
+    });
+    const float total =
+        __uint_as_float((uint32_t)lane_value((int)__float_as_uint(wave_scan(sum)), 63));
+    const uint32_t tiles = (uint32_t)lane_value((int)wave_scan(count), 63);
     // (q_start entries out of order can name more tiles than the launch has room for: no walk is
     // cut then, so that no merge waits for a piece that does not run)
     if (tiles <= (uint32_t)p.tiles) share = p.share_of(total);
   }
   uint32_t base = 0, sbase = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const Chunk c = b0 == 0 ? c0 : chunk(b0 + lane);
+  bool found = false;
+  round([&](int b0, const Chunk& c) {
     const int nt = p.tiles_of(c);
     const int ways = p.pieces_of(p.steps_of(a.shape, c), share);
-    const uint32_t count = (uint32_t)nt * (uint32_t)ways;
-    const uint32_t cut = ways > 1 ? count : 0u;
+    const uint32_t pieces = (uint32_t)nt * (uint32_t)ways;
+    const uint32_t cut = ways > 1 ? pieces : 0u;
+    const uint32_t count = !CUT ? pieces : ways > 1 ? (uint32_t)nt : 0u;
     const uint32_t upto = wave_scan(count), supto = wave_scan(cut);
     const uint32_t all = (uint32_t)lane_value((int)upto, 63);
-    if ((uint32_t)item < base + all) {
-      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)item < base + upto));
-      it.b = b0 + l;
-      it.c.row0 = lane_value(c.row0, l);
-      it.c.count = lane_value(c.count, l);
-      it.c.pos = lane_value(c.pos, l);
-      it.ways = lane_value(ways, l);
-      const int tiles = lane_value(nt, l);
-      const int r = item - (int)(base + (uint32_t)lane_value((int)(upto - count), l));
-      it.piece = r / tiles;
-      it.tile = tiles - 1 - (r - it.piece * tiles);
-      it.slot = (int)(sbase + (uint32_t)lane_value((int)(supto - cut), l)) + it.tile * it.ways;
+    if ((uint32_t)item >= base + all) {
+      base += all;
+      sbase += (uint32_t)lane_value((int)supto, 63);
       return true;
     }
-    base += all;
-    sbase += (uint32_t)lane_value((int)supto, 63);
-  }
-  return false;
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)item < base + upto));
+    it.b = b0 + l;
+    it.c.row0 = lane_value(c.row0, l);
+    it.c.count = lane_value(c.count, l);
+    it.c.pos = lane_value(c.pos, l);
+    it.ways = lane_value(ways, l);
+    const int tiles = lane_value(nt, l);
+    const int r = item - (int)(base + (uint32_t)lane_value((int)(upto - count), l));
+    it.piece = r / tiles;
+    it.tile = tiles - 1 - (r - it.piece * tiles);
+    it.slot = (int)(sbase + (uint32_t)lane_value((int)(supto - cut), l)) + it.tile * it.ways;
+    found = true;
+    return false;
+  });
+  return found;
 }
 
 // Merges the `ways` partial states of a tile ([COLS][D] outputs, then (reference, sum) per column,
@@ -147,6 +169,89 @@ __device__ __forceinline__ void merge_states(const float* s0, size_t stride, int
     store(col, 4 * q, o, l);
     if (q == 0) lse(col, m, l);
   }
+}
+
+// 1 / l and the natural-log partition of a column with reference m and sum l; an empty support has
+// l 0 and gets zeros and -inf.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float log_partition(float m, float l) {
+  return l == 0.0f ? kNegInf : (m + __builtin_log2f(l)) * 0.69314718055994531f;
+}
+
+__device__ __forceinline__ void store4(uint16_t* p, f32x4 o, float scale) {
+  *(u32x2*)p = u32x2{pack_bf16(o[0] * scale, o[1] * scale), pack_bf16(o[2] * scale, o[3] * scale)};
+}
+__device__ __forceinline__ void store4(float* p, f32x4 o, float scale) { *(f32x4*)p = o * scale; }
+
+// Merges the states of cut walks, a launch of its own after the pieces': x = (cut tile, KV head), y =
+// runs of 16 columns, four to a wave.  Lane l takes channels 64 i + 4 (l mod 16) .. +3 of column l / 16.
+template <typename T, int D, int COLS>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
+  constexpr int NB = D / 64;
+  constexpr int U = 8;   // states in flight
+  constexpr size_t STATE = paged_state_bytes(COLS, D) / 4;
+  const int lane = threadIdx.x & 63;
+  const PagedPlan& pl = a.plan;
+  const int item = pl.by_hkv.div((int)blockIdx.x);
+  const int g = (int)blockIdx.x - item * a.hkv;
+  PagedItem it;
+  if (!find_item<true>(a, item, lane, it) || it.c.pos < 0) return;
+  const int p0 = it.tile * pl.tq;
+  const int col = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 4);
+  if (col >= min(pl.tq, it.c.count - p0) * a.group) return;
+  const float* s = a.states + ((size_t)it.slot * a.hkv + (size_t)g * it.ways) * STATE;
+  const float* so = s + col * D + 4 * (lane & 15);
+  const float* sm = s + COLS * D + 2 * col;
+  float m = -3.0e38f, l = 0.0f;
+  f32x4 o[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto take = [&](auto states, int w0) {   // (a state read twice would need a weight of 0)
+    constexpr int N = decltype(states)::value;
+    float2 ml[N];
+    f32x4 x[N][NB];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      ml[u] = *(const float2*)(sm + (size_t)(w0 + u) * STATE);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) x[u][i] = *(const f32x4*)(so + (size_t)(w0 + u) * STATE + 64 * i);
+    }
+    float mx = m;
+#pragma unroll
+    for (int u = 0; u < N; ++u) mx = fmaxf(mx, ml[u].x);
+    const float keep = fast_exp2(m - mx);
+    l *= keep;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[i] *= keep;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const float wt = fast_exp2(ml[u].x - mx);
+      l += wt * ml[u].y;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o[i] += wt * x[u][i];
+    }
+    m = mx;
+  };
+  int w = 0;
+  for (; w + U <= it.ways; w += U) take(std::integral_constant<int, U>{}, w);
+  if (w + 4 <= it.ways) take(std::integral_constant<int, 4>{}, w), w += 4;
+  if (w + 2 <= it.ways) take(std::integral_constant<int, 2>{}, w), w += 2;
+  if (w < it.ways) take(std::integral_constant<int, 1>{}, w);
+  const int cp = pl.by_group.div(col);
+  const int64_t row = (int64_t)it.c.row0 + p0 + cp;
+  const int head = g * a.group + col - cp * a.group;
+  const float inv = inverse_sum(l);
+  T* out = (T*)a.out + (row * a.hq + head) * D + 4 * (lane & 15);
+#pragma unroll
+  for (int i = 0; i < NB; ++i) store4(out + 64 * i, o[i], inv);
+  if (a.lse != nullptr && (lane & 15) == 0) a.lse[(int64_t)head * a.n + row] = log_partition(m, l);
+}
+
+template <typename T, int D, int COLS>
+hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((paged_merge_kernel<T, D, COLS>),
+                     dim3((unsigned)(a.plan.cut_tiles() * a.hkv), COLS / 16), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace pbb

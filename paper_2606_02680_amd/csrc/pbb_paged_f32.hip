@@ -54,7 +54,7 @@ void paged_f32_kernel(PagedArgs a) {
   const int item = pl.by_hkv.div((int)blockIdx.x);
   const int g = (int)blockIdx.x - item * a.hkv;
   PagedItem it;
-  if (!find_item(a, item, lane, it)) return;
+  if (!find_item<false>(a, item, lane, it)) return;
   const int p0 = it.tile * pl.tq;
   const int tokens = min(pl.tq, it.c.count - p0);
   const int64_t row0 = (int64_t)it.c.row0 + p0;
@@ -84,6 +84,7 @@ void paged_f32_kernel(PagedArgs a) {
   const int t_last = t0 + tokens - 1;
   int s_first = sh.support_lo(t0) >> 4;
   int nsteps = max(0, (min(t_last, sh.capacity - 1) >> 4) - s_first + 1);
+  if (nsteps == 0) s_first = 0;   // (all past the table: positions whose next steps pass 2^31)
   if (it.ways > 1) {
     const int lo = (int)((int64_t)it.piece * nsteps / it.ways);
     const int hi = (int)((int64_t)(it.piece + 1) * nsteps / it.ways);
@@ -269,14 +270,10 @@ void paged_f32_kernel(PagedArgs a) {
   for (; st < nsteps; ++st) begin_step(st);
 
   // Lane (c16, j4) holds channels 64 y + 16 j4 + 4 i + x in acc[4 y + x][i].
-  auto inverse = [](float l) { return l == 0.0f ? 0.0f : 1.0f / l; };
-  auto log_partition = [](float mref, float l) {
-    return l == 0.0f ? kNegInf : (mref + __builtin_log2f(l)) * 0.69314718055994531f;
-  };
   const float l = sum_xor16_32(lsum);
   if (it.ways == 1) {
     if (valid) {
-      const float inv = inverse(l);
+      const float inv = inverse_sum(l);
       float* o = (float*)a.out + address(col) * D + 16 * j4;
 #pragma unroll
       for (int y = 0; y < E / 4; ++y)
@@ -289,9 +286,22 @@ void paged_f32_kernel(PagedArgs a) {
     return;
   }
 
-  constexpr size_t STATE = paged_state_bytes(kPagedColsF32, D) / 4;
+  const int scols = pl.narrow ? kPagedNarrowCols : kPagedColsF32;
+  const size_t STATE = paged_state_bytes(scols, D) / 4;
   const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;
   float* const part = a.states + (unit + it.piece) * STATE;
+  if (!pl.narrow) {   // (see the bf16 kernel)
+    if (valid) {
+#pragma unroll
+      for (int y = 0; y < E / 4; ++y)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(f32x4*)(part + col * D + 64 * y + 16 * j4 + 4 * i) =
+              f32x4{acc[4 * y][i], acc[4 * y + 1][i], acc[4 * y + 2][i], acc[4 * y + 3][i]};
+      if (j4 == 0) *(float2*)(part + scols * D + 2 * col) = make_float2(m, l);
+    }
+    return;
+  }
   if (valid) {
 #pragma unroll
     for (int y = 0; y < E / 4; ++y)
@@ -301,7 +311,7 @@ void paged_f32_kernel(PagedArgs a) {
         coherent_store2(o, acc[4 * y][i], acc[4 * y + 1][i]);
         coherent_store2(o + 2, acc[4 * y + 2][i], acc[4 * y + 3][i]);
       }
-    if (j4 == 0) coherent_store2(part + kPagedColsF32 * D + 2 * col, m, l);
+    if (j4 == 0) coherent_store2(part + scols * D + 2 * col, m, l);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
   __syncthreads();
@@ -314,10 +324,10 @@ void paged_f32_kernel(PagedArgs a) {
   }
   __syncthreads();
   if (!last_one) return;
-  merge_states<D, kPagedColsF32, NW * 64>(
+  merge_states<D, kPagedNarrowCols, NW * 64>(
       a.states + unit * STATE, STATE, it.ways, cols, tid,
       [&](int mc, int c, f32x4 o, float ml) {
-        *(f32x4*)((float*)a.out + address(mc) * D + c) = o * inverse(ml);
+        *(f32x4*)((float*)a.out + address(mc) * D + c) = o * inverse_sum(ml);
       },
       [&](int mc, float mref, float ml) {
         if (a.lse != nullptr) a.lse[lse_at(mc)] = log_partition(mref, ml);
@@ -326,13 +336,21 @@ void paged_f32_kernel(PagedArgs a) {
 
 }  // namespace
 
+namespace {
+
+template <int D>
+hipError_t launch_paged_t(const PagedArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((paged_f32_kernel<D>), dim3((unsigned)(a.plan.items() * a.hkv)),
+                     dim3(kF32Waves * 64), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.plan.pieces == 0 || a.plan.narrow) return e;
+  return launch_paged_merge<float, D, kPagedColsF32>(a, stream);
+}
+
+}  // namespace
+
 hipError_t launch_paged_f32(const PagedArgs& a, int32_t head_dim, hipStream_t stream) {
-  const unsigned blocks = (unsigned)(a.plan.items() * a.hkv);
-  if (head_dim == 64)
-    hipLaunchKernelGGL((paged_f32_kernel<64>), dim3(blocks), dim3(kF32Waves * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((paged_f32_kernel<128>), dim3(blocks), dim3(kF32Waves * 64), 0, stream, a);
-  return hipGetLastError();
+  return head_dim == 64 ? launch_paged_t<64>(a, stream) : launch_paged_t<128>(a, stream);
 }
 
 }  // namespace pbb

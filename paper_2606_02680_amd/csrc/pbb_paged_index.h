@@ -82,34 +82,73 @@ struct PagedShape {
 // (a sequence far longer than the others does not hold the call up), there are at most
 // tiles + pieces workgroups, and at most 2 x pieces of them belong to walks that are cut.  The
 // kernels work this out by themselves, from positions that only the device knows.
-constexpr int kPagedPieces = 1024;   // workgroups that a call's cut walks may add, in all heads
-constexpr int kPagedLeastSteps = 8;  // key steps of a piece, at least
+//
+// Calls of few columns per sequence (`narrow`: single tokens, short drafts) have kernels of their
+// own.  Their states are small, and the last piece of a walk to end merges them; states of 128
+// columns (66 KiB at d = 128) would keep one workgroup busy for 3 us each, so the others merge in a
+// second launch, four waves per 16 columns.
+constexpr int kPagedNarrowCols = 16;
+constexpr int kPagedMaxPieces = 2048;   // budget of a call's KV heads together, at most
+
+// Tile and cutting rules of a kind of kernel.
+struct PagedKind {
+  int cols;     // query columns of a tile
+  int step;     // keys per step
+  int slots;    // workgroups that a call of few tiles should have (0: every call has many)
+  // A call of fewer than twice as many tiles: pieces such that tiles and pieces together are that many
+  // (half as many pieces, where the tiles alone nearly are), of few_least steps at least.
+  int few_least;
+  // Others: many_pieces pieces (in all heads), of many_least steps at least.
+  int many_pieces, many_least;
+};
 
 struct PagedPlan {
+  int cols;      // query columns of a tile
   int tq;        // tokens per tile
+  int least;     // steps of a piece, at least
   int step;      // keys per step
   int pieces;    // budget per KV head; 0: no walk is cut
   int uniform;   // tokens of every sequence, -1: q_start says
+  int narrow;    // 1: at most kPagedNarrowCols columns per sequence
+  int few;       // 1: a call of few tiles
   int tiles;     // tiles of a call, at most
   int slots;     // partial states per KV head, at most
   FastDiv by_hkv, by_tq, by_group;
-  static PagedPlan make(const PagedShape& s, int batch, int hkv, int group, int n_tokens,
-                        bool ragged, int cols, int step) {
+  static bool is_narrow(int batch, int group, int n_tokens, bool ragged) {
+    return !ragged && (int64_t)(n_tokens / batch) * group <= kPagedNarrowCols;
+  }
+  static PagedPlan make(const PagedShape& s, const PagedKind& k, int batch, int hkv, int group,
+                        int n_tokens, bool ragged) {
     PagedPlan p;
-    p.tq = cols / group;
-    p.step = step;
     p.uniform = ragged ? -1 : n_tokens / batch;
+    p.narrow = is_narrow(batch, group, n_tokens, ragged);
+    p.cols = k.cols;
+    p.tq = p.cols / group;
+    p.step = k.step;
     p.by_hkv = FastDiv::make((uint32_t)hkv);
     p.by_tq = FastDiv::make((uint32_t)p.tq);
     p.by_group = FastDiv::make((uint32_t)group);
     // ceil(n / tq) of every sequence, summed: at most one more each than of all together
     p.tiles = ragged ? n_tokens / p.tq + (batch < n_tokens ? batch : n_tokens)
                      : batch * ((p.uniform + p.tq - 1) / p.tq);
+    const int held = k.slots / hkv;   // of a KV head
+    p.few = p.tiles < 2 * held;
+    p.least = p.few ? k.few_least : k.many_least;
+    const int budget = !p.few ? k.many_pieces / hkv : held - p.tiles > held / 2 ? held - p.tiles : held / 2;
     const int64_t keys = s.max_keys(s.capacity, p.tq);
-    const int64_t longest = (keys + step - 1) / step + 1;
-    p.pieces = longest > kPagedLeastSteps && 2 * hkv <= kPagedPieces ? kPagedPieces / hkv : 0;
+    const int64_t longest = (keys + p.step - 1) / p.step + 1;
+    p.pieces = longest > p.least && 2 * hkv <= kPagedMaxPieces ? budget : 0;
     p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
     return p;
+  }
+  // (Partial states of a head over all calls of a kind.)
+  static int max_slots(const PagedShape& s, const PagedKind& k, int hkv, int tq) {
+    const int64_t keys = s.max_keys(s.capacity, tq);
+    const int64_t longest = (keys + k.step - 1) / k.step + 1;
+    const int least = k.few_least < k.many_least ? k.few_least : k.many_least;
+    if (longest <= least || 2 * hkv > kPagedMaxPieces) return 0;
+    const int p = (k.slots > k.many_pieces ? k.slots : k.many_pieces) / hkv;
+    return p > 0 ? 2 * p + p / 8 + 2 : 0;
   }
   // Tiles of a chunk, and the longest walk of one of them in steps.
   PBB_HD int tiles_of(const Chunk& c) const { return c.count > 0 ? by_tq.div(c.count - 1) + 1 : 0; }
@@ -126,8 +165,10 @@ struct PagedPlan {
   }
   PBB_HD float share_of(float total) const {
     const float c = pieces > 0 ? total / (float)pieces : 0.0f;
-    return c > (float)kPagedLeastSteps ? c : (float)kPagedLeastSteps;
+    return c > (float)least ? c : (float)least;
   }
+  // Tiles per KV head whose walks are cut, at most (each is longer than an even share).
+  int cut_tiles() const { return tiles < pieces + pieces / 16 + 1 ? tiles : pieces + pieces / 16 + 1; }
   // Workgroups per KV head, at most.
   int64_t items() const { return (int64_t)tiles + pieces + pieces / 16 + 1; }
 };

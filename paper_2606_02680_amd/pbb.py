@@ -480,7 +480,7 @@ def paged_workspace_bytes(desc: PbbPagedDesc, n_tokens: int) -> int:
     return out.value
 
 
-PAGED_COUNTER_BYTES = 16384
+PAGED_COUNTER_BYTES = 65536
 
 
 def alloc_paged_workspace(desc: PbbPagedDesc, n_tokens: int, device="cuda"):

@@ -466,7 +466,7 @@ def test_graph_replays(cuda, dtype):
         step(y, eager, own)
         assert torch.equal(out, eager), i
         assert torch.equal(x["k_pages"], y["k_pages"])
-    assert not bool(ws[:16384].any()) and not bool(own[:16384].any())
+    assert not bool(ws[:P.pbb.PAGED_COUNTER_BYTES].any()) and not bool(own[:P.pbb.PAGED_COUNTER_BYTES].any())
 
 
 def test_side_stream_and_own_workspace(cuda):
@@ -496,7 +496,7 @@ def test_writes_only_its_buffers(cuda, dtype):
     qo, out = (Guarded((c.n, 12, 64), dtype, cuda) for _ in range(2))
     lse = Guarded((12, c.n), F32, cuda)
     ws = Guarded(None, torch.uint8, cuda, nbytes=P.paged_workspace_bytes(desc, c.n))
-    ws.t[:16384].zero_()
+    ws.t[:P.pbb.PAGED_COUNTER_BYTES].zero_()
     before = {n: t.clone() for n, t in x.items()}
     print(f"[guard] {dtype}", flush=True)
     P.pbb_paged_append(desc, x["pos"], x["table"], x["k"], x["v"], kg.t, vg.t, q_start=x["q_start"],
