@@ -181,13 +181,18 @@ struct PagedArgs {
 constexpr int kPagedCols = 128, kPagedStep = 32;          // bf16
 constexpr int kPagedColsF32 = 64, kPagedStepF32 = 16;     // fp32
 inline PagedKind paged_kind(bool f32, bool narrow, int head_dim) {
-  if (f32) return PagedKind{narrow ? kPagedNarrowCols : kPagedColsF32, kPagedStepF32, 768, 8, 1024, 32};
-  // Single tokens: one workgroup per CU where there are few (d = 128; 32/8 heads, one sequence of
-  // 32000 28.2 us, against 32.4 and 36.7 for two and three per CU; eight of up to 8000 30.3 / 31.2 /
-  // 32.9).  Many: pieces of fewer than 64 steps cost more than an even end gains (256 sequences of
-  // up to 600: 73 us, 115 with pieces of 8); 2048 of them, not 1024 (192 of up to 32768: 1870 / 1934).
+  // Few columns.  One round is one workgroup per CU at d = 128 (32/8 heads: one sequence of 32000 28.0
+  // us, 33.2 with half as many again; eight of up to 8000 30.7 / 34.3; tiles and pieces over one round
+  // 37), two at d = 64, and two of the fp32 kernel's register-bound ones.  Shares of 64 steps and more
+  // are cut by the second rule: 2048 pieces (192 sequences of up to 32768: 1875, 1934 with 1024) of 64
+  // steps (256 of up to 600: 71; pieces of 8: 115), in fp32 32 of 16 keys (256 of up to 2000, 16/2
+  // heads: 125 / 134 with 64).
+  if (f32 && narrow) return PagedKind{kPagedNarrowCols, kPagedStepF32, 512, 8, 2048, 32};
   if (narrow) return PagedKind{kPagedNarrowCols, kPagedStep, head_dim == 64 ? 512 : 256, 8, 2048, 64};
-  return PagedKind{kPagedCols, kPagedStep, 0, 32, 1024, 32};
+  // Many columns: states are large, pieces of fewer than 32 steps cost more than they gain (512 tokens
+  // of four prompts 28.7 us, 50 with 16; 128 tokens behind 16000 57, 69 with 64 steps).
+  if (f32) return PagedKind{kPagedColsF32, kPagedStepF32, 0, 0, 2048, 32};
+  return PagedKind{kPagedCols, kPagedStep, 0, 0, 1024, 32};
 }
 constexpr size_t kPagedCounterBytes = 65536;
 

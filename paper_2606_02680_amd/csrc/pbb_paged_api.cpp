@@ -89,8 +89,9 @@ size_t workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
   size_t bytes = 0;
   for (const bool narrow : {false, true}) {
     const pbb::PagedKind k = pbb::paged_kind(d->dtype == PBB_DTYPE_F32, narrow, d->head_dim);
-    const size_t need = (size_t)pbb::PagedPlan::max_slots(s, k, d->n_kv_heads, k.cols / group) *
-                        d->n_kv_heads * pbb::paged_state_bytes(k.cols, d->head_dim);
+    const pbb::PagedPlan p = pbb::PagedPlan::make(s, k, d->batch, d->n_kv_heads, group, d->batch, true);
+    const size_t need =
+        (size_t)p.slots * d->n_kv_heads * pbb::paged_state_bytes(k.cols, d->head_dim);
     bytes = need > bytes ? need : bytes;
   }
   return bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;

@@ -50,8 +50,10 @@ struct PagedItem {
 
 // Item `item` of a KV head (false: there are not that many).  Every wave finds it by itself, 64
 // sequences at a time: their counts of pieces, and a sum over the lanes.  Items go sequence by
-// sequence; of one sequence, piece by piece from the last tile (the longest walk) to the first, so
-// that workgroups running side by side read the same keys.  CUT: the items are the tiles whose walks
+// sequence, those of more than kPagedNarrowCols columns first (their pieces take longest: behind the
+// others, two chunks of 620 tokens among 128 single ones ended a call of 267 us that takes 260 so); of
+// one sequence, piece by piece from the last tile (the longest walk) to the first, so that workgroups
+// running side by side read the same keys.  CUT: the items are the tiles whose walks
 // are cut (piece 0).
 template <bool CUT>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane, PagedItem& it) {
@@ -95,33 +97,41 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
   }
   uint32_t base = 0, sbase = 0;
   bool found = false;
-  round([&](int b0, const Chunk& c) {
-    const int nt = p.tiles_of(c);
-    const int ways = p.pieces_of(p.steps_of(a.shape, c), share);
-    const uint32_t pieces = (uint32_t)nt * (uint32_t)ways;
-    const uint32_t cut = ways > 1 ? pieces : 0u;
-    const uint32_t count = !CUT ? pieces : ways > 1 ? (uint32_t)nt : 0u;
-    const uint32_t upto = wave_scan(count), supto = wave_scan(cut);
-    const uint32_t all = (uint32_t)lane_value((int)upto, 63);
-    if ((uint32_t)item >= base + all) {
-      base += all;
-      sbase += (uint32_t)lane_value((int)supto, 63);
-      return true;
-    }
-    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)item < base + upto));
-    it.b = b0 + l;
-    it.c.row0 = lane_value(c.row0, l);
-    it.c.count = lane_value(c.count, l);
-    it.c.pos = lane_value(c.pos, l);
-    it.ways = lane_value(ways, l);
-    const int tiles = lane_value(nt, l);
-    const int r = item - (int)(base + (uint32_t)lane_value((int)(upto - count), l));
-    it.piece = r / tiles;
-    it.tile = tiles - 1 - (r - it.piece * tiles);
-    it.slot = (int)(sbase + (uint32_t)lane_value((int)(supto - cut), l)) + it.tile * it.ways;
-    found = true;
-    return false;
-  });
+  auto search = [&](auto&& mine) {   // among the sequences that mine(tokens) takes
+    round([&](int b0, const Chunk& c) {
+      const int nt = mine(c.count) ? p.tiles_of(c) : 0;
+      const int ways = p.pieces_of(p.steps_of(a.shape, c), share);
+      const uint32_t pieces = (uint32_t)nt * (uint32_t)ways;
+      const uint32_t cut = ways > 1 ? pieces : 0u;
+      const uint32_t count = !CUT ? pieces : ways > 1 ? (uint32_t)nt : 0u;
+      const uint32_t upto = wave_scan(count), supto = wave_scan(cut);
+      const uint32_t all = (uint32_t)lane_value((int)upto, 63);
+      if ((uint32_t)item >= base + all) {
+        base += all;
+        sbase += (uint32_t)lane_value((int)supto, 63);
+        return true;
+      }
+      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)item < base + upto));
+      it.b = b0 + l;
+      it.c.row0 = lane_value(c.row0, l);
+      it.c.count = lane_value(c.count, l);
+      it.c.pos = lane_value(c.pos, l);
+      it.ways = lane_value(ways, l);
+      const int tiles = lane_value(nt, l);
+      const int r = item - (int)(base + (uint32_t)lane_value((int)(upto - count), l));
+      it.piece = r / tiles;
+      it.tile = tiles - 1 - (r - it.piece * tiles);
+      it.slot = (int)(sbase + (uint32_t)lane_value((int)(supto - cut), l)) + it.tile * it.ways;
+      found = true;
+      return false;
+    });
+  };
+  if (p.uniform >= 0) {
+    search([](int) { return true; });
+  } else {
+    search([&](int count) { return count * a.group > kPagedNarrowCols; });
+    if (!found) search([&](int count) { return count * a.group <= kPagedNarrowCols; });
+  }
   return found;
 }
 

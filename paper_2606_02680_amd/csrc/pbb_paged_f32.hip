@@ -26,6 +26,286 @@ __device__ __forceinline__ bool is_special(float x) {
   return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
 }
 
+// Few columns: tiles of at most 16.  The 16-key steps of a piece are dealt to the waves one by one;
+// a wave reads its rows straight into registers as operands (as the fp32 decode does: 64 contiguous
+// bytes of each of 16 key rows, 256 of each of 4 value rows per 16-byte load), the next step's loads in
+// flight while it computes.  Bound: HBM, by the register loads that 8 waves per CU hold in flight.
+constexpr int kF32Merge128 = kF32Waves * kPagedNarrowCols * (128 + 2) * 4 + 16;
+
+template <int D, bool IN_PLACE>
+__device__ __forceinline__ void narrow_walk_f32(const PagedArgs& a, const PagedItem& it, int g,
+                                                unsigned char* smem) {
+  constexpr int NW = kF32Waves;
+  constexpr int KM = D / 4;
+  constexpr int E = D / 16;
+  constexpr int KQ = KM / 4;    // 16-byte loads of a lane's key channels
+  constexpr int VQ = E / 4;     // and of each of its four value rows
+  constexpr int ROWB = D * 4;
+  constexpr int COLS = kPagedNarrowCols;
+  constexpr int MERGE = NW * COLS * (D + 2) * 4;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15;
+  const int j4 = lane >> 4;
+  const int G = a.group;
+  const PagedPlan& pl = a.plan;
+  const PagedShape& sh = a.shape;
+  const int tokens = it.c.count;
+  const int64_t row0 = it.c.row0;
+  const int cols = tokens * G;
+  auto address = [&](int col) -> int64_t {   // output row of a column
+    const int cp = pl.by_group.div(col);
+    return (row0 + cp) * a.hq + (int64_t)(g * G + col - cp * G);
+  };
+  auto lse_at = [&](int col) -> int64_t {
+    const int cp = pl.by_group.div(col);
+    return (int64_t)(g * G + col - cp * G) * a.n + row0 + cp;
+  };
+  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
+    if (it.piece > 0) return;
+    for (int i = tid; i < cols * (D / 4); i += NW * 64) {
+      const int col = i / (D / 4);
+      *(f32x4*)((float*)a.out + address(col) * D + (i - col * (D / 4)) * 4) =
+          f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    if (a.lse != nullptr && tid < cols) a.lse[lse_at(tid)] = kNegInf;
+    return;
+  }
+
+  const int t0 = it.c.pos;
+  const int t_last = t0 + tokens - 1;
+  int s0 = sh.support_lo(t0) >> 4;
+  int nsteps = max(0, (min(t_last, sh.capacity - 1) >> 4) - s0 + 1);
+  if (nsteps == 0) s0 = 0;   // (all past the table: positions whose next steps pass 2^31)
+  if (it.ways > 1) {
+    const int lo = (int)((int64_t)it.piece * nsteps / it.ways);
+    const int hi = (int)((int64_t)(it.piece + 1) * nsteps / it.ways);
+    s0 += lo;
+    nsteps = hi - lo;
+  }
+  const int s1 = s0 + nsteps;   // steps [s0, s1): keys 16 s .. +15
+
+  const int cp = min(pl.by_group.div(c16), tokens - 1);
+  const bool valid = c16 < cols;
+  const int tcol = valid ? t0 + cp : -1;
+  const int lo_c = sh.support_lo(t0 + cp);
+  float qf[KM];
+  {
+    const float* qrow = (const float*)((const unsigned char*)a.q + (row0 + cp) * a.q_stride +
+                                       (int64_t)(g * G + (valid ? c16 - cp * G : 0)) * ROWB) + 4 * j4;
+#pragma unroll
+    for (int x = 0; x < KM / 4; ++x) {
+      const f32x4 v = *(const f32x4*)(qrow + 16 * x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qf[4 * x + e] = valid ? v[e] * a.scale_log2 : 0.0f;
+    }
+  }
+
+  const int32_t* const table = a.table + (size_t)it.b * sh.width;
+  const uint32_t page_bytes = (uint32_t)sh.page_size * ROWB;   // of one KV head
+  const uint64_t page_stride = (uint64_t)page_bytes * (uint32_t)a.hkv;
+  const unsigned char* const keys = (const unsigned char*)a.k_pages + (uint64_t)page_bytes * (uint32_t)g;
+  const unsigned char* const values = (const unsigned char*)a.v_pages + (uint64_t)page_bytes * (uint32_t)g;
+  struct Entry { int id; uint32_t slot; };
+  auto fetch = [&](int st) -> Entry {
+    const int i = min(sh.by_page.div(16 * st), sh.width - 1);
+    return Entry{scalar_word(table, i), (uint32_t)(16 * st - i * sh.page_size) * ROWB};
+  };
+  auto load = [&](const Entry& e, f32x4 (&kb)[KQ], f32x4 (&vb)[4][VQ]) __attribute__((always_inline)) {
+    const uint64_t off = (sh.is_page(e.id) ? (uint32_t)e.id : 0u) * page_stride + e.slot;
+    const unsigned char* kp = keys + off + (uint32_t)(c16 * ROWB + 16 * j4);
+    const unsigned char* vp = values + off + (uint32_t)(4 * j4 * ROWB + 16 * c16);
+#pragma unroll
+    for (int q = 0; q < KQ; ++q) kb[q] = __builtin_nontemporal_load((const f32x4*)(kp + 64 * q));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int q = 0; q < VQ; ++q)
+        vb[k][q] = __builtin_nontemporal_load((const f32x4*)(vp + k * ROWB + 256 * q));
+  };
+  // steps whose keys all lie in every column's support
+  const int ua = (sh.support_lo(t_last) + 15) >> 4;
+  const int ub = (t0 + 1) >> 4;
+
+  float m = valid ? kNoScore : 0.0f, lsum = 0.0f;
+  f32x4 acc[E];
+#pragma unroll
+  for (int nb = 0; nb < E; ++nb) acc[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  bool first = true;
+
+  auto compute = [&](int st, bool gone, const f32x4 (&kb)[KQ], const f32x4 (&vb)[4][VQ])
+      __attribute__((always_inline)) {
+    f32x4 sp[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sp[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < KM; ++i)
+      sp[i & 7] = __builtin_amdgcn_mfma_f32_16x16x4f32(kb[i >> 2][i & 3], qf[i], sp[i & 7], 0, 0, 0);
+    f32x4 s = ((sp[0] + sp[1]) + (sp[2] + sp[3])) + ((sp[4] + sp[5]) + (sp[6] + sp[7]));
+    const bool masked = st < ua || st >= ub || gone;
+    const int k0 = 16 * st + 4 * j4;
+    bool sees[4] = {true, true, true, true};
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sees[e] = e >= lo_c - k0 && e <= tcol - k0 && !gone;
+        s[e] = sees[e] ? s[e] : kNegInf;
+      }
+    }
+    const float mx = max_xor16_32(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+    const bool grow = mx > m + 8.0f || (first && mx > m);
+    first = false;
+    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+      const float alpha = grow ? fast_exp2(m - mx) : 1.0f;
+      m = grow ? mx : m;
+      lsum *= alpha;
+#pragma unroll
+      for (int nb = 0; nb < E; ++nb) acc[nb] *= alpha;
+    }
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = fast_exp2(s[e] - m);
+    lsum += (p[0] + p[1]) + (p[2] + p[3]);
+    bool odd = false;
+    if (masked) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int q = 0; q < VQ; ++q)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) odd |= is_special(vb[k][q][x]);
+    }
+    const bool apart = masked && __builtin_amdgcn_ballot_w64(odd) != 0;
+#pragma unroll
+    for (int nb = 0; nb < E; ++nb) {
+      f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (!apart) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          part = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[k][nb >> 2][nb & 3], p[k], part, 0, 0, 0);
+      } else {   // infinities and NaN, counted for the columns that see their key
+        f32x4 cu = {0.0f, 0.0f, 0.0f, 0.0f}, cd = cu;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float w = vb[k][nb >> 2][nb & 3], one = sees[k] ? 1.0f : 0.0f;
+          const bool sp1 = is_special(w), nan = w != w;
+          cu = __builtin_amdgcn_mfma_f32_16x16x4f32(sp1 && (nan || w > 0.0f) ? 1.0f : 0.0f, one, cu, 0, 0, 0);
+          cd = __builtin_amdgcn_mfma_f32_16x16x4f32(sp1 && (nan || w < 0.0f) ? 1.0f : 0.0f, one, cd, 0, 0, 0);
+          part = __builtin_amdgcn_mfma_f32_16x16x4f32(sp1 ? 0.0f : w, p[k], part, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          part[e] += (cu[e] > 0.0f ? -kNegInf : 0.0f) + (cd[e] > 0.0f ? kNegInf : 0.0f);
+      }
+      acc[nb] += part;
+    }
+  };
+
+  f32x4 ka[KQ], kb[KQ], va[4][VQ], vb[4][VQ];
+  int st = s0 + wave;
+  if (st < s1) {
+    Entry e0 = fetch(st), e1 = fetch(min(st + NW, s1 - 1));
+    load(e0, ka, va);
+    while (true) {
+      const bool g0 = !sh.is_page(e0.id);
+      if (st + NW < s1) load(e1, kb, vb);
+      e0 = fetch(min(st + 2 * NW, s1 - 1));
+      compute(st, g0, ka, va);
+      st += NW;
+      if (st >= s1) break;
+      const bool g1 = !sh.is_page(e1.id);
+      if (st + NW < s1) load(e0, ka, va);
+      e1 = fetch(min(st + 2 * NW, s1 - 1));
+      compute(st, g1, kb, vb);
+      st += NW;
+      if (st >= s1) break;
+    }
+  }
+
+  // The waves' states through LDS (Eq.(lse)).
+  lsum = sum_xor16_32(lsum);
+  float* const sm_acc = (float*)smem;               // [NW][COLS][D]
+  float* const sm_m = sm_acc + NW * COLS * D;       // [NW][COLS]
+  float* const sm_l = sm_m + NW * COLS;
+  int* const last_one = (int*)(smem + MERGE);
+#pragma unroll
+  for (int y = 0; y < E / 4; ++y)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(f32x4*)(sm_acc + (wave * COLS + c16) * D + 64 * y + 16 * j4 + 4 * i) =
+          f32x4{acc[4 * y][i], acc[4 * y + 1][i], acc[4 * y + 2][i], acc[4 * y + 3][i]};
+  if (j4 == 0) {
+    sm_m[wave * COLS + c16] = m;
+    sm_l[wave * COLS + c16] = lsum;
+  }
+  __syncthreads();
+  constexpr int SCOLS = IN_PLACE ? COLS : kPagedColsF32;
+  constexpr size_t STATE = paged_state_bytes(SCOLS, D) / 4;
+  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
+  float* const part = a.states + (unit + it.piece) * STATE;
+  for (int i = tid; i < cols * (D / 4); i += NW * 64) {
+    const int col = i / (D / 4), q = i - col * (D / 4);
+    float M = kNoScore;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * COLS + col]);
+    float L = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {   // (a wave that saw nothing holds zeros)
+      const float wt = fast_exp2(sm_m[w * COLS + col] - M);
+      L += wt * sm_l[w * COLS + col];
+      o += wt * *(const f32x4*)(sm_acc + (w * COLS + col) * D + 4 * q);
+    }
+    if (it.ways == 1) {
+      store4((float*)a.out + address(col) * D + 4 * q, o, inverse_sum(L));
+      if (a.lse != nullptr && q == 0) a.lse[lse_at(col)] = log_partition(M, L);
+    } else if (IN_PLACE) {
+      coherent_store2(part + col * D + 4 * q, o[0], o[1]);
+      coherent_store2(part + col * D + 4 * q + 2, o[2], o[3]);
+      if (q == 0) coherent_store2(part + SCOLS * D + 2 * col, M, L);
+    } else {
+      *(f32x4*)(part + col * D + 4 * q) = o;
+      if (q == 0) *(float2*)(part + SCOLS * D + 2 * col) = make_float2(M, L);
+    }
+  }
+  if (!IN_PLACE || it.ways == 1) return;
+  // A cut walk: whoever completes the count of its pieces merges them (coherent_store2 says why this
+  // orders).
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+    *last_one = before == (unsigned)(it.ways - 1);
+    if (*last_one)
+      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!*last_one) return;
+  merge_states<D, SCOLS, NW * 64>(
+      a.states + unit * STATE, STATE, it.ways, cols, tid,
+      [&](int col, int c, f32x4 o, float l) {
+        store4((float*)a.out + address(col) * D + c, o, inverse_sum(l));
+      },
+      [&](int col, float mref, float l) {
+        if (a.lse != nullptr) a.lse[lse_at(col)] = log_partition(mref, l);
+      });
+}
+
+template <int D>
+__global__ __launch_bounds__(kF32Waves * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void paged_narrow_f32_kernel(PagedArgs a) {
+  __shared__ __align__(1024) unsigned char smem[kF32Merge128];
+  const int lane = threadIdx.x & 63;
+  const int item = a.plan.by_hkv.div((int)blockIdx.x);
+  const int g = (int)blockIdx.x - item * a.hkv;
+  PagedItem it;
+  if (!find_item<false>(a, item, lane, it)) return;
+  narrow_walk_f32<D, true>(a, it, g, smem);
+}
+
 template <int D>
 __global__ __launch_bounds__(kF32Waves * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_f32_kernel(PagedArgs a) {
@@ -40,7 +320,6 @@ void paged_f32_kernel(PagedArgs a) {
   constexpr int STAGES = kF32Stages;
   constexpr int OPS = BUF / 1024 / NW;  // DMA instructions of a wave per step
   __shared__ __align__(1024) unsigned char smem[STAGES * BUF];
-  __shared__ int last_one;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -55,6 +334,11 @@ void paged_f32_kernel(PagedArgs a) {
   const int g = (int)blockIdx.x - item * a.hkv;
   PagedItem it;
   if (!find_item<false>(a, item, lane, it)) return;
+  if (it.c.count * G <= kPagedNarrowCols) {
+    static_assert(sizeof(smem) >= kF32Waves * kPagedNarrowCols * (D + 2) * 4, "LDS");
+    narrow_walk_f32<D, false>(a, it, g, smem);
+    return;
+  }
   const int p0 = it.tile * pl.tq;
   const int tokens = min(pl.tq, it.c.count - p0);
   const int64_t row0 = (int64_t)it.c.row0 + p0;
@@ -286,52 +570,18 @@ void paged_f32_kernel(PagedArgs a) {
     return;
   }
 
-  const int scols = pl.narrow ? kPagedNarrowCols : kPagedColsF32;
-  const size_t STATE = paged_state_bytes(scols, D) / 4;
-  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;
-  float* const part = a.states + (unit + it.piece) * STATE;
-  if (!pl.narrow) {   // (see the bf16 kernel)
-    if (valid) {
-#pragma unroll
-      for (int y = 0; y < E / 4; ++y)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *(f32x4*)(part + col * D + 64 * y + 16 * j4 + 4 * i) =
-              f32x4{acc[4 * y][i], acc[4 * y + 1][i], acc[4 * y + 2][i], acc[4 * y + 3][i]};
-      if (j4 == 0) *(float2*)(part + scols * D + 2 * col) = make_float2(m, l);
-    }
-    return;
-  }
+  constexpr size_t STATE = paged_state_bytes(kPagedColsF32, D) / 4;
+  float* const part =
+      a.states + ((size_t)it.slot * a.hkv + (size_t)g * it.ways + it.piece) * STATE;
   if (valid) {
 #pragma unroll
     for (int y = 0; y < E / 4; ++y)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float* o = part + col * D + 64 * y + 16 * j4 + 4 * i;
-        coherent_store2(o, acc[4 * y][i], acc[4 * y + 1][i]);
-        coherent_store2(o + 2, acc[4 * y + 2][i], acc[4 * y + 3][i]);
-      }
-    if (j4 == 0) coherent_store2(part + scols * D + 2 * col, m, l);
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(part + col * D + 64 * y + 16 * j4 + 4 * i) =
+            f32x4{acc[4 * y][i], acc[4 * y + 1][i], acc[4 * y + 2][i], acc[4 * y + 3][i]};
+    if (j4 == 0) *(float2*)(part + kPagedColsF32 * D + 2 * col) = make_float2(m, l);
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
-  __syncthreads();
-  if (tid == 0) {
-    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-    last_one = before == (unsigned)(it.ways - 1);
-    if (last_one)
-      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!last_one) return;
-  merge_states<D, kPagedNarrowCols, NW * 64>(
-      a.states + unit * STATE, STATE, it.ways, cols, tid,
-      [&](int mc, int c, f32x4 o, float ml) {
-        *(f32x4*)((float*)a.out + address(mc) * D + c) = o * inverse_sum(ml);
-      },
-      [&](int mc, float mref, float ml) {
-        if (a.lse != nullptr) a.lse[lse_at(mc)] = log_partition(mref, ml);
-      });
 }
 
 }  // namespace
@@ -340,10 +590,14 @@ namespace {
 
 template <int D>
 hipError_t launch_paged_t(const PagedArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_f32_kernel<D>), dim3((unsigned)(a.plan.items() * a.hkv)),
-                     dim3(kF32Waves * 64), 0, stream, a);
+  const dim3 grid((unsigned)(a.plan.items() * a.hkv));
+  if (a.plan.narrow) {
+    hipLaunchKernelGGL((paged_narrow_f32_kernel<D>), grid, dim3(kF32Waves * 64), 0, stream, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((paged_f32_kernel<D>), grid, dim3(kF32Waves * 64), 0, stream, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.plan.pieces == 0 || a.plan.narrow) return e;
+  if (e != hipSuccess || a.plan.pieces == 0) return e;
   return launch_paged_merge<float, D, kPagedColsF32>(a, stream);
 }
 

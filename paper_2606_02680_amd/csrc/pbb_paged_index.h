@@ -90,27 +90,28 @@ struct PagedShape {
 constexpr int kPagedNarrowCols = 16;
 constexpr int kPagedMaxPieces = 2048;   // budget of a call's KV heads together, at most
 
-// Tile and cutting rules of a kind of kernel.
+// Tile and cutting rules of a kind of kernel.  Where the even share of one round of the chip is short
+// (below many_least), C is that share, at least few_least: T / (round - tiles), so that tiles and pieces
+// together are no more than the round (half of the round, where the tiles alone are that many).  Else C = max(many_least, T / pieces): as many pieces as even out the end of the call, but
+// none so short that its first loads and its merge cost more than that gains.
 struct PagedKind {
   int cols;     // query columns of a tile
   int step;     // keys per step
-  int slots;    // workgroups that a call of few tiles should have (0: every call has many)
-  // A call of fewer than twice as many tiles: pieces such that tiles and pieces together are that many
-  // (half as many pieces, where the tiles alone nearly are), of few_least steps at least.
+  int round;    // workgroups of one round, in all heads (0: always the second rule)
   int few_least;
-  // Others: many_pieces pieces (in all heads), of many_least steps at least.
-  int many_pieces, many_least;
+  int pieces;   // in all heads
+  int many_least;
 };
 
 struct PagedPlan {
   int cols;      // query columns of a tile
   int tq;        // tokens per tile
-  int least;     // steps of a piece, at least
   int step;      // keys per step
-  int pieces;    // budget per KV head; 0: no walk is cut
+  int pieces;    // pieces of cut walks per KV head, at most; 0: no walk is cut
+  int few_least, many_least;
+  float per_round, per_pieces;   // 1 / workgroups of a round, 1 / pieces, per KV head
   int uniform;   // tokens of every sequence, -1: q_start says
   int narrow;    // 1: at most kPagedNarrowCols columns per sequence
-  int few;       // 1: a call of few tiles
   int tiles;     // tiles of a call, at most
   int slots;     // partial states per KV head, at most
   FastDiv by_hkv, by_tq, by_group;
@@ -131,24 +132,19 @@ struct PagedPlan {
     // ceil(n / tq) of every sequence, summed: at most one more each than of all together
     p.tiles = ragged ? n_tokens / p.tq + (batch < n_tokens ? batch : n_tokens)
                      : batch * ((p.uniform + p.tq - 1) / p.tq);
-    const int held = k.slots / hkv;   // of a KV head
-    p.few = p.tiles < 2 * held;
-    p.least = p.few ? k.few_least : k.many_least;
-    const int budget = !p.few ? k.many_pieces / hkv : held - p.tiles > held / 2 ? held - p.tiles : held / 2;
-    const int64_t keys = s.max_keys(s.capacity, p.tq);
-    const int64_t longest = (keys + p.step - 1) / p.step + 1;
-    p.pieces = longest > p.least && 2 * hkv <= kPagedMaxPieces ? budget : 0;
+    const int all = k.round / hkv, many = k.pieces / hkv;
+    const int round = all - (p.tiles < all / 2 ? p.tiles : all / 2);
+    p.few_least = round > 0 ? k.few_least : k.many_least;
+    p.many_least = k.many_least;
+    p.per_round = 1.0f / (float)(round > 0 ? round : 1);
+    p.per_pieces = 1.0f / (float)(many > 0 ? many : 1);
+    p.pieces = longest_walk(s, k, p.tq) > p.few_least && 2 * hkv <= kPagedMaxPieces
+                   ? (round > many ? round : many) : 0;
     p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
     return p;
   }
-  // (Partial states of a head over all calls of a kind.)
-  static int max_slots(const PagedShape& s, const PagedKind& k, int hkv, int tq) {
-    const int64_t keys = s.max_keys(s.capacity, tq);
-    const int64_t longest = (keys + k.step - 1) / k.step + 1;
-    const int least = k.few_least < k.many_least ? k.few_least : k.many_least;
-    if (longest <= least || 2 * hkv > kPagedMaxPieces) return 0;
-    const int p = (k.slots > k.many_pieces ? k.slots : k.many_pieces) / hkv;
-    return p > 0 ? 2 * p + p / 8 + 2 : 0;
+  static int64_t longest_walk(const PagedShape& s, const PagedKind& k, int tq) {
+    return (s.max_keys(s.capacity, tq) + k.step - 1) / k.step + 1;
   }
   // Tiles of a chunk, and the longest walk of one of them in steps.
   PBB_HD int tiles_of(const Chunk& c) const { return c.count > 0 ? by_tq.div(c.count - 1) + 1 : 0; }
@@ -164,8 +160,10 @@ struct PagedPlan {
     return p > 1 ? p : 1;
   }
   PBB_HD float share_of(float total) const {
-    const float c = pieces > 0 ? total / (float)pieces : 0.0f;
-    return c > (float)least ? c : (float)least;
+    const float one = total * per_round, many = total * per_pieces;
+    const float least = (float)many_least;
+    if (few_least < many_least && one < least) return one > (float)few_least ? one : (float)few_least;
+    return many > least ? many : least;
   }
   // Tiles per KV head whose walks are cut, at most (each is longer than an even share).
   int cut_tiles() const { return tiles < pieces + pieces / 16 + 1 ? tiles : pieces + pieces / 16 + 1; }
