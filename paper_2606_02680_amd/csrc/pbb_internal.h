@@ -125,7 +125,9 @@ struct RotateArgs {
   int64_t x_stride, out_stride;
   int32_t n;
   int32_t heads;
-  int32_t run;                // heads per grid row (set by the launcher)
+  int32_t run;                // heads per grid row (this and the next two set by the launcher)
+  int32_t tokens_per_wave;
+  FastDiv by_heads;
   RopeArgs rope;              // negative rates turn backwards
 };
 

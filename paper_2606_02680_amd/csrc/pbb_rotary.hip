@@ -82,22 +82,26 @@ __device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&
   hi = Piece<T>::put(oy);
 }
 
-// Grid: x = tokens / waves per workgroup, y = runs of a token's heads.
+// Grid: x = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token has
+// fewer heads than a wave takes rows, a wave takes several tokens (2 heads, d 64, 16000 tokens with 12
+// query heads: 20.9 us for both calls with one token per wave, 15.9 with eight).
 template <typename T, int D>
 __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   constexpr int PC = D * (int)sizeof(T) / 32;   // pieces per half row
   constexpr int ROWS = 64 / PC;                 // rows of a wave at a time
   constexpr int ROWB = D * (int)sizeof(T);
   const int lane = threadIdx.x & 63;
-  const int64_t tok = (int64_t)blockIdx.x * (kRotThreads / 64) + (threadIdx.x >> 6);
-  if (tok >= a.n) return;
+  const int row = lane / PC;
+  const int sub = a.tokens_per_wave > 1 ? a.by_heads.div(row) : 0;   // token within the wave's
+  const int64_t tok = ((int64_t)blockIdx.x * (kRotThreads / 64) + (threadIdx.x >> 6)) * a.tokens_per_wave + sub;
+  if (tok >= a.n || sub >= a.tokens_per_wave) return;
   const int pc = lane % PC;
   float cs[Piece<T>::N], sn[Piece<T>::N];
   piece_turns<T>(a.rope, pc, [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; }, cs, sn);
   const unsigned char* x = (const unsigned char*)a.x + tok * a.x_stride + pc * 16;
   unsigned char* o = (unsigned char*)a.out + tok * a.out_stride + pc * 16;
   const int h1 = min(a.heads, (int)(blockIdx.y + 1) * a.run);
-  for (int h = blockIdx.y * a.run + lane / PC; h < h1; h += ROWS) {
+  for (int h = blockIdx.y * a.run + row - sub * a.heads; h < h1; h += ROWS) {
     const unsigned char* p = x + (size_t)h * ROWB;
     u32x4 lo = *(const u32x4*)p, hi = *(const u32x4*)(p + ROWB / 2);
     turn_pieces<T>(lo, hi, cs, sn);
@@ -189,10 +193,13 @@ int head_run(int tokens, int heads, int rows) {
 
 template <typename T, int D>
 hipError_t rotate_t(const RotateArgs& a0, hipStream_t stream) {
+  constexpr int ROWS = 64 / (D * (int)sizeof(T) / 32), WAVES = kRotThreads / 64;
   RotateArgs a = a0;
-  a.run = head_run(a.n, a.heads, 64 / (D * (int)sizeof(T) / 32));
-  const dim3 grid((unsigned)((a.n + kRotThreads / 64 - 1) / (kRotThreads / 64)),
-                  (unsigned)((a.heads + a.run - 1) / a.run));
+  a.by_heads = FastDiv::make((uint32_t)a.heads);
+  a.tokens_per_wave = a.heads < ROWS ? ROWS / a.heads : 1;
+  a.run = a.heads < ROWS ? a.heads : head_run(a.n, a.heads, ROWS);
+  const int per = WAVES * a.tokens_per_wave;
+  const dim3 grid((unsigned)(((int64_t)a.n + per - 1) / per), (unsigned)((a.heads + a.run - 1) / a.run));
   hipLaunchKernelGGL((rotate_kernel<T, D>), grid, dim3(kRotThreads), 0, stream, a);
   return hipGetLastError();
 }

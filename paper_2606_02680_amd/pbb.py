@@ -406,12 +406,15 @@ def make_rope(head_dim: int, base: float, axis=None) -> PbbRope:
     return rope
 
 
-def _expect_rows(name: str, t: torch.Tensor, shape, dtype) -> int:
+def _rows(name: str, t: torch.Tensor, shape, dtype, device: int) -> int:
     """Checks packed rows [tokens][heads][d] whose tokens may lie apart; returns their stride."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor")
-    if t.device.type != "cuda":
-        raise ValueError(f"{name}: must be a GPU tensor, got {t.device}")
+    # the usual case in few expressions (0.5 us, against 1.5 for the checks one by one)
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == device):
+        s = t.stride()
+        if s[2] == 1 and s[1] == shape[2]:
+            return s[0] if shape[0] > 1 else shape[1] * shape[2]
+    _expect_on(name, t, device)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
     if t.dtype != dtype:
@@ -422,13 +425,38 @@ def _expect_rows(name: str, t: torch.Tensor, shape, dtype) -> int:
     return t.stride(0) if n > 1 else heads * d
 
 
-def _expect_on(device, **tensors):
-    """Checks that a call's tensors lie on one device, the current one (whose streams it uses)."""
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name}: on {t.device}, expected {device}")
+def _expect_on(name: str, t: torch.Tensor, device: int):
+    """Checks that a call's tensor lies on the current device (whose streams the call uses)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: must be a GPU tensor, got {t.device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{device}")
+
+
+def _dense(name: str, t: torch.Tensor, shape, dtype, device: int):
+    """:func:`_expect` of a tensor on the current device."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == device and t.is_contiguous()):
+        return
+    _expect_on(name, t, device)
+    _expect(name, t, shape, dtype)
+
+
+def _device_for(name: str, t: torch.Tensor, rows: str) -> int:
+    """The current device, for a call whose first tensor of rows is ``t``."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name}: must be {rows}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a GPU tensor, got {t.device}")
+    return torch.cuda.current_device()
+
+
+def _stream_on(stream, device: int) -> int:
+    if stream is None and _current_raw_stream is not None:
+        return _current_raw_stream(device)
+    return _stream(stream)
 
 
 def pbb_rotate(rope: PbbRope, positions: torch.Tensor, x: torch.Tensor, out: torch.Tensor,
@@ -436,20 +464,22 @@ def pbb_rotate(rope: PbbRope, positions: torch.Tensor, x: torch.Tensor, out: tor
     """Turn rows ``x`` [tokens][heads][d] by ``positions`` (int32 [axes][tokens], or [tokens] for one
     axis) into ``out``; ``inverse`` turns gradients back.  Tokens may lie apart (a part of a fused
     projection buffer); ``out`` may be ``x``."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 3:
-        raise ValueError("x: must be [tokens][heads][d]")
+    dev = _device_for("x", x, "[tokens][heads][d]")
     n, heads, _ = x.shape
-    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}.get(x.dtype, -1)
+    dtype = x.dtype
+    code = DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_F32 if dtype is torch.float32 else -1
     shape = (n, heads, rope.head_dim)
-    xs, os_ = _expect_rows("x", x, shape, x.dtype), _expect_rows("out", out, shape, x.dtype)
-    if rope.n_axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1:
-        _expect("positions", positions, (n,), torch.int32)
+    xs, outs = _rows("x", x, shape, dtype, dev), _rows("out", out, shape, dtype, dev)
+    axes = rope.n_axes
+    if axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1:
+        _dense("positions", positions, (n,), torch.int32, dev)
     else:
-        _expect("positions", positions, (rope.n_axes, n), torch.int32)
-    _expect_on(x.device, out=out, positions=positions)
-    _check("pbb_rotate", load_library().pbb_rotate(
-        ctypes.byref(rope), n, heads, _ptr(positions), _ptr(x), xs, _ptr(out), os_, int(inverse), code,
-        _stream(stream)))
+        _dense("positions", positions, (axes, n), torch.int32, dev)
+    status = load_library().pbb_rotate(
+        rope, n, heads, positions.data_ptr(), x.data_ptr(), xs, out.data_ptr(), outs, inverse, code,
+        _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_rotate", status)
     return out
 
 
@@ -495,14 +525,17 @@ def alloc_paged_workspace(desc: PbbPagedDesc, n_tokens: int, device="cuda"):
     return ws
 
 
-def _expect_paged(desc: PbbPagedDesc, n: int, pos, table, q_start, k_pages, v_pages):
-    _expect("pos", pos, (desc.batch,), torch.int32)
-    _expect("table", table, (desc.batch, desc.table_width), torch.int32)
+def _expect_paged(desc: PbbPagedDesc, pos, table, q_start, k_pages, v_pages, dev: int):
+    """The tensor checks that append and attention share; returns (Hq, Hkv, d, dtype)."""
+    batch, hkv, d, dtype = desc.batch, desc.n_kv_heads, desc.head_dim, desc.torch_dtype
+    _dense("pos", pos, (batch,), torch.int32, dev)
+    _dense("table", table, (batch, desc.table_width), torch.int32, dev)
     if q_start is not None:
-        _expect("q_start", q_start, (desc.batch + 1,), torch.int32)
-    shape, dtype = pages_shape(desc), desc.torch_dtype
-    _expect("k_pages", k_pages, shape, dtype)
-    _expect("v_pages", v_pages, shape, dtype)
+        _dense("q_start", q_start, (batch + 1,), torch.int32, dev)
+    shape = (desc.n_pages, hkv, desc.page_size, d)
+    _dense("k_pages", k_pages, shape, dtype, dev)
+    _dense("v_pages", v_pages, shape, dtype, dev)
+    return desc.n_q_heads, hkv, d, dtype
 
 
 def pbb_paged_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, q_start=None, rope=None,
@@ -510,28 +543,26 @@ def pbb_paged_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, q_s
     """Append the new tokens of every sequence to the cache (see ``include/pbb.h``): ``k``, ``v``
     [tokens][Hkv][d] packed by ``q_start`` (None: the same number for every sequence), ``rope``
     applied to ``k`` and, into ``q_out``, to ``q`` [tokens][Hq][d]."""
-    if not isinstance(k, torch.Tensor) or k.dim() != 3:
-        raise ValueError("k: must be [tokens][Hkv][d]")
-    n, dtype = k.shape[0], desc.torch_dtype
-    _expect_paged(desc, n, pos, table, q_start, k_pages, v_pages)
-    kv = (n, desc.n_kv_heads, desc.head_dim)
-    ks, vs, qs = _expect_rows("k", k, kv, dtype), _expect_rows("v", v, kv, dtype), 0
+    dev = _device_for("k", k, "[tokens][Hkv][d]")
+    n = k.shape[0]
+    hq, hkv, d, dtype = _expect_paged(desc, pos, table, q_start, k_pages, v_pages, dev)
+    kv = (n, hkv, d)
+    ks, vs, qs = _rows("k", k, kv, dtype, dev), _rows("v", v, kv, dtype, dev), 0
     if (q is None) != (q_out is None):
         raise ValueError("pbb_paged_append: pass both q and q_out or neither")
     if q is not None:
-        heads = (n, desc.n_q_heads, desc.head_dim)
-        qs = _expect_rows("q", q, heads, dtype)
-        _expect("q_out", q_out, heads, dtype)
+        qs = _rows("q", q, (n, hq, d), dtype, dev)
+        _dense("q_out", q_out, (n, hq, d), dtype, dev)
     if rope_pos is not None:
         if rope is None:
             raise ValueError("pbb_paged_append: rope_pos without rope")
-        _expect("rope_pos", rope_pos, (rope.n_axes, n), torch.int32)
-    _expect_on(k.device, pos=pos, table=table, q_start=q_start, k_pages=k_pages, v_pages=v_pages, v=v,
-               q=q, q_out=q_out, rope_pos=rope_pos)
-    _check("pbb_paged_append", load_library().pbb_paged_append(
-        ctypes.byref(desc), n, _ptr(pos), _ptr(q_start), _ptr(table),
-        None if rope is None else ctypes.byref(rope), _ptr(rope_pos), _ptr(q), qs, _ptr(q_out),
-        _ptr(k), ks, _ptr(v), vs, _ptr(k_pages), _ptr(v_pages), _stream(stream)))
+        _dense("rope_pos", rope_pos, (rope.n_axes, n), torch.int32, dev)
+    status = load_library().pbb_paged_append(
+        desc, n, pos.data_ptr(), _ptr(q_start), table.data_ptr(), rope, _ptr(rope_pos), _ptr(q), qs,
+        _ptr(q_out), k.data_ptr(), ks, v.data_ptr(), vs, k_pages.data_ptr(), v_pages.data_ptr(),
+        _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_paged_append", status)
 
 
 def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out, q_start=None,
@@ -539,21 +570,24 @@ def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out
     """Attention of the new tokens over the cache that holds them (see ``include/pbb.h``): ``q``,
     ``out`` [tokens][Hq][d] packed by ``q_start``; optional ``lse`` [Hq][tokens] (float32).
     Allocates the workspace when none is given."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise ValueError("q: must be [tokens][Hq][d]")
-    n, dtype = q.shape[0], desc.torch_dtype
-    _expect_paged(desc, n, pos, table, q_start, k_pages, v_pages)
-    heads = (n, desc.n_q_heads, desc.head_dim)
-    qs = _expect_rows("q", q, heads, dtype)
-    _expect("out", out, heads, dtype)
+    dev = _device_for("q", q, "[tokens][Hq][d]")
+    n = q.shape[0]
+    hq, _, d, dtype = _expect_paged(desc, pos, table, q_start, k_pages, v_pages, dev)
+    qs = _rows("q", q, (n, hq, d), dtype, dev)
+    _dense("out", out, (n, hq, d), dtype, dev)
     if lse is not None:
-        _expect("lse", lse, (desc.n_q_heads, n), torch.float32)
-    _expect_on(q.device, pos=pos, table=table, q_start=q_start, k_pages=k_pages, v_pages=v_pages,
-               out=out, lse=lse, workspace=workspace)
-    if workspace is None and paged_workspace_bytes(desc, n) > 0:
+        _dense("lse", lse, (hq, n), torch.float32, dev)
+    ws_bytes = 0
+    if workspace is not None:
+        _expect_on("workspace", workspace, dev)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    elif paged_workspace_bytes(desc, n) > 0:
         workspace = _scratch_on(stream, lambda: alloc_paged_workspace(desc, n, q.device))
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check("pbb_paged_attention", load_library().pbb_paged_attention(
-        ctypes.byref(desc), n, _ptr(pos), _ptr(q_start), _ptr(table), _ptr(q), qs, _ptr(k_pages),
-        _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)))
+        ws_bytes = workspace.numel()
+    status = load_library().pbb_paged_attention(
+        desc, n, pos.data_ptr(), _ptr(q_start), table.data_ptr(), q.data_ptr(), qs, k_pages.data_ptr(),
+        v_pages.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(workspace), ws_bytes,
+        _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_paged_attention", status)
     return out
