@@ -50,11 +50,11 @@ struct PagedItem {
 
 // Item `item` of a KV head (false: there are not that many).  Every wave finds it by itself, 64
 // sequences at a time: their counts of pieces, and a sum over the lanes.  Items go sequence by
-// sequence, those of more than kPagedNarrowCols columns first (their pieces take longest: behind the
-// others, two chunks of 620 tokens among 128 single ones ended a call of 267 us that takes 260 so); of
-// one sequence, piece by piece from the last tile (the longest walk) to the first, so that workgroups
-// running side by side read the same keys.  CUT: the items are the tiles whose walks
-// are cut (piece 0).
+// sequence, those of more than kPagedNarrowCols columns first, whose pieces take longest (128 single
+// tokens and chunks of 665 and 577: 249 us, 267 in the sequences' order, 303 with both kinds in turn,
+// eight items of each); of one sequence, piece by piece from the last tile (the longest walk) to the
+// first, so that workgroups running side by side read the same keys.  CUT: the items are the tiles
+// whose walks are cut (piece 0).
 template <bool CUT>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane, PagedItem& it) {
   const PagedPlan& p = a.plan;

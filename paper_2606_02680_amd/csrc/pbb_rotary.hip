@@ -17,6 +17,11 @@ namespace pbb {
 namespace {
 
 constexpr int kRotThreads = 256;
+// Rows of more bytes than the last-level cache (256 MB) are read and written with the non-temporal
+// hint: what is written first is gone before anything reads it (4 x 16384 tokens of 32 heads, d 128:
+// 537 MB, 259 us with the 8 key heads' call, 235 with the hint, 5.7 TB/s; 16000 tokens, 131 MB: the
+// next kernel finds them in the cache).
+constexpr int64_t kStreamBytes = 256ll << 20;
 
 template <typename T>
 struct Piece;   // 16 bytes of a row as floats
@@ -85,7 +90,7 @@ __device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&
 // Grid: x = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token has
 // fewer heads than a wave takes rows, a wave takes several tokens (2 heads, d 64, 16000 tokens with 12
 // query heads: 20.9 us for both calls with one token per wave, 15.9 with eight).
-template <typename T, int D>
+template <typename T, int D, bool NT>
 __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   constexpr int PC = D * (int)sizeof(T) / 32;   // pieces per half row
   constexpr int ROWS = 64 / PC;                 // rows of a wave at a time
@@ -103,11 +108,19 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   const int h1 = min(a.heads, (int)(blockIdx.y + 1) * a.run);
   for (int h = blockIdx.y * a.run + row - sub * a.heads; h < h1; h += ROWS) {
     const unsigned char* p = x + (size_t)h * ROWB;
-    u32x4 lo = *(const u32x4*)p, hi = *(const u32x4*)(p + ROWB / 2);
-    turn_pieces<T>(lo, hi, cs, sn);
     unsigned char* w = o + (size_t)h * ROWB;
-    *(u32x4*)w = lo;
-    *(u32x4*)(w + ROWB / 2) = hi;
+    if constexpr (NT) {
+      u32x4 lo = __builtin_nontemporal_load((const u32x4*)p);
+      u32x4 hi = __builtin_nontemporal_load((const u32x4*)(p + ROWB / 2));
+      turn_pieces<T>(lo, hi, cs, sn);
+      __builtin_nontemporal_store(lo, (u32x4*)w);
+      __builtin_nontemporal_store(hi, (u32x4*)(w + ROWB / 2));
+    } else {
+      u32x4 lo = *(const u32x4*)p, hi = *(const u32x4*)(p + ROWB / 2);
+      turn_pieces<T>(lo, hi, cs, sn);
+      *(u32x4*)w = lo;
+      *(u32x4*)(w + ROWB / 2) = hi;
+    }
   }
 }
 
@@ -160,33 +173,47 @@ __global__ __launch_bounds__(kRotThreads) void paged_append_kernel(AppendArgs a)
   const int hq = a.q != nullptr ? a.hq : 0;
   const int rows = hq + 2 * a.hkv;
   const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
-  for (int r = blockIdx.y * a.run + lane / PC; r < r1; r += ROWS) {
-    const unsigned char* p;
-    unsigned char* w;
-    if (r < hq) {
-      p = (const unsigned char*)a.q + tok * a.q_stride + (size_t)r * ROWB;
-      w = (unsigned char*)a.q_out + ((size_t)tok * hq + r) * ROWB;
-    } else {
-      const bool key = r < hq + a.hkv;
-      const int h = r - hq - (key ? 0 : a.hkv);
-      p = (key ? (const unsigned char*)a.k + tok * a.k_stride
-               : (const unsigned char*)a.v + tok * a.v_stride) + (size_t)h * ROWB;
-      if (page < 0) continue;
-      w = (unsigned char*)(key ? a.k_pages : a.v_pages) +
-          (((size_t)page * a.hkv + h) * a.shape.page_size + slot) * ROWB;
+  constexpr int AU = 2;   // rows of a lane in flight (one: 49.5 us at 37 sequences' 9000 tokens, two 47)
+  const int64_t page_row = page < 0 ? 0 : (int64_t)page * a.hkv * a.shape.page_size + slot;
+  for (int r0 = blockIdx.y * a.run + lane / PC; r0 < r1; r0 += AU * ROWS) {
+    u32x4 lo[AU], hi[AU];
+#pragma unroll
+    for (int u = 0; u < AU; ++u) {
+      const int r = min(r0 + u * ROWS, r1 - 1);
+      const unsigned char* p =
+          (r < hq ? (const unsigned char*)a.q + tok * a.q_stride + (size_t)r * ROWB
+           : r < hq + a.hkv ? (const unsigned char*)a.k + tok * a.k_stride + (size_t)(r - hq) * ROWB
+                            : (const unsigned char*)a.v + tok * a.v_stride +
+                                  (size_t)(r - hq - a.hkv) * ROWB) + pc * 16;
+      lo[u] = *(const u32x4*)p, hi[u] = *(const u32x4*)(p + ROWB / 2);
     }
-    u32x4 lo = *(const u32x4*)(p + pc * 16), hi = *(const u32x4*)(p + pc * 16 + ROWB / 2);
-    if (a.turn && r < hq + a.hkv) turn_pieces<T>(lo, hi, cs, sn);
-    if (skip) lo = hi = u32x4{0u, 0u, 0u, 0u};
-    *(u32x4*)(w + pc * 16) = lo;
-    *(u32x4*)(w + pc * 16 + ROWB / 2) = hi;
+#pragma unroll
+    for (int u = 0; u < AU; ++u) {
+      const int r = r0 + u * ROWS;
+      if (r >= r1) break;
+      if (a.turn && r < hq + a.hkv) turn_pieces<T>(lo[u], hi[u], cs, sn);
+      unsigned char* w;
+      if (r < hq) {
+        if (skip) lo[u] = hi[u] = u32x4{0u, 0u, 0u, 0u};
+        w = (unsigned char*)a.q_out + ((size_t)tok * hq + r) * ROWB;
+      } else {
+        if (page < 0) break;
+        const bool key = r < hq + a.hkv;
+        const int h = r - hq - (key ? 0 : a.hkv);
+        w = (unsigned char*)(key ? a.k_pages : a.v_pages) +
+            (size_t)(page_row + (int64_t)h * a.shape.page_size) * ROWB;
+      }
+      *(u32x4*)(w + pc * 16) = lo[u];
+      *(u32x4*)(w + pc * 16 + ROWB / 2) = hi[u];
+    }
   }
 }
 
 // Heads per workgroup row of the grid: all of a token's, unless the tokens alone leave the chip
-// short of waves; then as few as a wave takes at once (and no more than 65535 runs).
+// short of waves; then as few as a wave takes at once, and no more than 65535 runs (2000 tokens of 48
+// rows: 11.5 us, 13.5 with a run per 8 rows; 256 tokens: 5.0 us so).
 int head_run(int tokens, int heads, int rows) {
-  if (tokens >= 4096) return heads;
+  if (tokens >= 1024) return heads;
   const int least = (heads + 65534) / 65535;
   return rows > least ? rows : least;
 }
@@ -200,7 +227,11 @@ hipError_t rotate_t(const RotateArgs& a0, hipStream_t stream) {
   a.run = a.heads < ROWS ? a.heads : head_run(a.n, a.heads, ROWS);
   const int per = WAVES * a.tokens_per_wave;
   const dim3 grid((unsigned)(((int64_t)a.n + per - 1) / per), (unsigned)((a.heads + a.run - 1) / a.run));
-  hipLaunchKernelGGL((rotate_kernel<T, D>), grid, dim3(kRotThreads), 0, stream, a);
+  const int64_t bytes = (int64_t)a.n * a.heads * D * (int64_t)sizeof(T);
+  if (bytes > kStreamBytes)
+    hipLaunchKernelGGL((rotate_kernel<T, D, true>), grid, dim3(kRotThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((rotate_kernel<T, D, false>), grid, dim3(kRotThreads), 0, stream, a);
   return hipGetLastError();
 }
 
