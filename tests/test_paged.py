@@ -67,6 +67,22 @@ def test_rotate(cuda, dtype, d, heads, n, axes):
         assert (bits(same) == bits(out)).all()
 
 
+@pytest.mark.parametrize("dtype,d,heads,n", [(BF, 64, 40, 60001), (F32, 128, 16, 40003)])
+def test_rotate_large(cuda, dtype, d, heads, n):
+    """Rows of more bytes than the last-level cache: the bits of calls on slices of them."""
+    g = torch.Generator(device=cuda).manual_seed(5)
+    x = torch.randn(n, heads, d, generator=g, device=cuda).to(dtype)
+    pos = torch.randint(0, 1 << 19, (2, n), generator=g, device=cuda).to(torch.int32)
+    rope = P.make_rope(d, BASE, _axis(d, 2))
+    assert x.numel() * x.element_size() > 256 << 20
+    print(f"[rotate] large {dtype}", flush=True)
+    out, parts = P.pbb_rotate(rope, pos, x, torch.empty_like(x)), torch.empty_like(x)
+    for i in range(0, n, 20000):
+        e = slice(i, min(n, i + 20000))
+        P.pbb_rotate(rope, pos[:, e].contiguous(), x[e], parts[e])
+    assert torch.equal(out, parts)
+
+
 def test_rotate_is_its_gradient(cuda):
     """<R x, y> = <x, R^T y> for random x, y, and R^T R x = x, in fp32; the same gradient by
     differences: (f(x + h e) - f(x - h e)) / 2h of f(x) = <R x, y>, exact for a linear f."""
@@ -221,6 +237,11 @@ def test_append_without_rotation_and_without_pages(cuda, dtype):
                        q_start=x["q_start"])
     assert (bits(x["k_pages"]) == bits(want["k"].to(dtype))).all()
     assert (bits(x["v_pages"]) == bits(want["v"].to(dtype))).all()
+    q_out = torch.empty_like(x["q"])
+    P.pbb_paged_append(c.desc(), x["pos"], x["table"], x["k"], x["v"], x["k_pages"], x["v_pages"],
+                       q_start=x["q_start"], q=x["q"], q_out=q_out)
+    assert torch.equal(q_out, x["q"])
+    assert (bits(x["k_pages"]) == bits(want["k"].to(dtype))).all()
 
 
 # ------------------------------------------------------------------------------------------
@@ -276,12 +297,66 @@ def test_attention_tokens(cuda, dtype, d, hq, hkv, page, lens, block, window):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,hq,hkv,page,lens,ragged", [
+    (128, 4, 1, 16, [(200, 4)] * 3, False),                     # 16 columns: few; ragged, the same rows
+    (128, 4, 1, 16, [(200, 4)] * 3, True),
+    (64, 5, 1, 48, [(1600, 3), (90, 4), (700, 3)], True),       # 15 columns: few, 20: many
+    (64, 1, 1, 16, [(1200, 16), (33, 17), (1, 1)], True),       # one head per KV head
+    (128, 16, 1, 32, [(1300, 1), (200, 2), (64, 1)], True),     # groups of 16
+    (64, 2, 2, 16, [(1000, 129)], True),                        # a column past a tile
+])
+def test_attention_column_limits(cuda, dtype, d, hq, hkv, page, lens, ragged):
+    c = Cache(lens, hq, hkv, d, page, dtype, seed=hq, uniform=not ragged, fill=math.nan)
+    _check(c, cuda)
+    _check(c, cuda, window=300)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("lens", [[(1000, 100)], [(0, 300)], [(513, 150), (3, 1), (640, 1), (20, 40)]])
 @pytest.mark.parametrize("d,hq,hkv,page,block,window", [(128, 4, 1, 16, 0, 0), (64, 6, 2, 48, 0, 0),
                                                         (128, 3, 1, 64, 256, 0), (64, 8, 1, 16, 0, 333)])
 def test_attention_chunks(cuda, dtype, lens, d, hq, hkv, page, block, window):
     _check(Cache(lens, hq, hkv, d, page, dtype, seed=d + hq, fill=-math.inf), cuda, block, window,
            scale=0.2 if hq == 3 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_many_sequences(cuda, dtype):
+    """More sequences than a wave keeps in registers (256): single tokens, one long walk among them, and
+    a ragged mixture with skipped and empty sequences."""
+    lens = [((i * 13) % 40, 1) for i in range(699)] + [(1200, 1)]
+    _check(Cache(lens, 2, 1, 64, 16, dtype, seed=15, uniform=True, fill=math.nan), cuda)
+    lens = [(-1 if i % 50 == 7 else (i * 13) % 40, (1, 1, 0, 3)[i % 4]) for i in range(500)]
+    lens[440], lens[3] = (300, 90), (500, 12)
+    _check(Cache(lens, 4, 2, 64, 16, dtype, seed=16, before=3, behind=1, fill=math.nan), cuda)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_q_start_out_of_order(cuda, dtype):
+    """q_start entries out of range or falling: no access leaves a buffer, no counter stays, and what a
+    sequence of whole entries brings is right."""
+    lens = [(500, 40), (700, 1), (900, 60), (0, 5)]
+    c = Cache(lens, 8, 2, 64, 16, dtype, seed=17)
+    x = c.on(cuda)
+    desc = c.desc()
+    good, _ = _attend(c, cuda, x=x)
+    ws = P.alloc_paged_workspace(desc, c.n, cuda)
+    out = Guarded(tuple(x["q"].shape), dtype, cuda, fill=torch.zeros_like(x["q"]))
+    lse = Guarded((8, c.n), F32, cuda)
+    for bad in ([0, 40, 41, 2000000000, 2147483647], [-5, 40, 41, 101, 106], [0, 40, 30, 101, 106],
+                [106, 0, 106, 0, 106], [0, -2147483648, 106, 106, 106]):
+        start = torch.tensor(bad, dtype=torch.int32, device=cuda)
+        kp, vp = x["k_pages"].clone(), x["v_pages"].clone()
+        print(f"[q_start] {dtype} {bad}", flush=True)
+        P.pbb_paged_append(desc, x["pos"], x["table"], x["k"], x["v"], kp, vp, q_start=start)
+        P.pbb_paged_attention(desc, x["pos"], x["table"], x["q"], x["k_pages"], x["v_pages"], out.t,
+                              q_start=start, lse=lse.t, workspace=ws)
+        torch.cuda.synchronize()
+        assert out.intact() and lse.intact()
+        assert not bool(ws[:P.pbb.PAGED_COUNTER_BYTES].any())
+    P.pbb_paged_attention(desc, x["pos"], x["table"], x["q"], x["k_pages"], x["v_pages"], out.t,
+                          q_start=x["q_start"], lse=lse.t, workspace=ws)
+    assert torch.equal(out.t, good)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -467,6 +542,57 @@ def test_graph_replays(cuda, dtype):
         assert torch.equal(out, eager), i
         assert torch.equal(x["k_pages"], y["k_pages"])
     assert not bool(ws[:P.pbb.PAGED_COUNTER_BYTES].any()) and not bool(own[:P.pbb.PAGED_COUNTER_BYTES].any())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_graph_of_chunks(cuda, dtype):
+    """A ragged call (walks cut, a second launch merges them) captured and replayed with new data in
+    its buffers: every replay against the eager call."""
+    c = Cache([(1500, 20), (40, 1), (2500, 1), (600, 70)], 8, 2, 64, 16, dtype, seed=18)
+    x = c.on(cuda)
+    desc, rope = c.desc(), P.make_rope(64, BASE)
+    ws = P.alloc_paged_workspace(desc, c.n, cuda)
+    assert ws is not None
+    q_out, out = torch.empty_like(x["q"]), torch.empty_like(x["q"])
+
+    def step(o, w):
+        P.pbb_paged_append(desc, x["pos"], x["table"], x["k"], x["v"], x["k_pages"], x["v_pages"],
+                           q_start=x["q_start"], rope=rope, q=x["q"], q_out=q_out)
+        P.pbb_paged_attention(desc, x["pos"], x["table"], q_out, x["k_pages"], x["v_pages"], o,
+                              q_start=x["q_start"], workspace=w)
+
+    print(f"[graph] chunks {dtype}", flush=True)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(out, ws)
+    eager = torch.empty_like(out)
+    for i in range(5):
+        x["q"].copy_(x["q"].roll(1, 0))
+        x["v"].copy_(x["v"].roll(1, 2))
+        x["pos"][2] += 3 if i < 3 else -5
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager, None)
+        assert torch.equal(out, eager), i
+
+
+def test_two_streams(cuda):
+    """Two calls at once on streams and workspaces of their own."""
+    cs = [Cache([(3000, 1), (700, 40)], 8, 2, 128, 16, BF, seed=s) for s in (19, 20)]
+    xs = [c.on(cuda) for c in cs]
+    refs = [_attend(c, cuda, x=x)[0] for c, x in zip(cs, xs)]
+    streams = [torch.cuda.Stream() for _ in cs]
+    ws = [P.alloc_paged_workspace(c.desc(), c.n, cuda) for c in cs]
+    outs = [torch.empty_like(r) for r in refs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, x, s, w, o in zip(cs, xs, streams, ws, outs):
+            P.pbb_paged_attention(c.desc(), x["pos"], x["table"], x["q"], x["k_pages"], x["v_pages"], o,
+                                  q_start=x["q_start"], workspace=w, stream=s)
+    torch.cuda.synchronize()
+    for r, o in zip(refs, outs):
+        assert torch.equal(r, o)
 
 
 def test_side_stream_and_own_workspace(cuda):
