@@ -194,7 +194,8 @@ __device__ __forceinline__ void store4(uint16_t* p, f32x4 o, float scale) {
 __device__ __forceinline__ void store4(float* p, f32x4 o, float scale) { *(f32x4*)p = o * scale; }
 
 // Merges the states of cut walks, a launch of its own after the pieces': x = (cut tile, KV head), y =
-// runs of 16 columns, four to a wave.  Lane l takes channels 64 i + 4 (l mod 16) .. +3 of column l / 16.
+// runs of 16 columns (in turn where the grid has fewer), four to a wave.  Lane l takes channels
+// 64 i + 4 (l mod 16) .. +3 of column l / 16.
 template <typename T, int D, int COLS>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   constexpr int NB = D / 64;
@@ -207,60 +208,64 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   PagedItem it;
   if (!find_item<true>(a, item, lane, it) || it.c.pos < 0) return;
   const int p0 = it.tile * pl.tq;
-  const int col = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 4);
-  if (col >= min(pl.tq, it.c.count - p0) * a.group) return;
+  const int cols = min(pl.tq, it.c.count - p0) * a.group;
   const float* s = a.states + ((size_t)it.slot * a.hkv + (size_t)g * it.ways) * STATE;
-  const float* so = s + col * D + 4 * (lane & 15);
-  const float* sm = s + COLS * D + 2 * col;
-  float m = -3.0e38f, l = 0.0f;
-  f32x4 o[NB];
+  for (int col = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 4); col < cols; col += (int)gridDim.y * 16) {
+    const float* so = s + col * D + 4 * (lane & 15);
+    const float* sm = s + COLS * D + 2 * col;
+    float m = -3.0e38f, l = 0.0f;
+    f32x4 o[NB];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  auto take = [&](auto states, int w0) {   // (a state read twice would need a weight of 0)
-    constexpr int N = decltype(states)::value;
-    float2 ml[N];
-    f32x4 x[N][NB];
+    for (int i = 0; i < NB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto take = [&](auto states, int w0) {   // (a state read twice would need a weight of 0)
+      constexpr int N = decltype(states)::value;
+      float2 ml[N];
+      f32x4 x[N][NB];
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      ml[u] = *(const float2*)(sm + (size_t)(w0 + u) * STATE);
+      for (int u = 0; u < N; ++u) {
+        ml[u] = *(const float2*)(sm + (size_t)(w0 + u) * STATE);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) x[u][i] = *(const f32x4*)(so + (size_t)(w0 + u) * STATE + 64 * i);
-    }
-    float mx = m;
+        for (int i = 0; i < NB; ++i) x[u][i] = *(const f32x4*)(so + (size_t)(w0 + u) * STATE + 64 * i);
+      }
+      float mx = m;
 #pragma unroll
-    for (int u = 0; u < N; ++u) mx = fmaxf(mx, ml[u].x);
-    const float keep = fast_exp2(m - mx);
-    l *= keep;
+      for (int u = 0; u < N; ++u) mx = fmaxf(mx, ml[u].x);
+      const float keep = fast_exp2(m - mx);
+      l *= keep;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) o[i] *= keep;
+      for (int i = 0; i < NB; ++i) o[i] *= keep;
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const float wt = fast_exp2(ml[u].x - mx);
-      l += wt * ml[u].y;
+      for (int u = 0; u < N; ++u) {
+        const float wt = fast_exp2(ml[u].x - mx);
+        l += wt * ml[u].y;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) o[i] += wt * x[u][i];
-    }
-    m = mx;
-  };
-  int w = 0;
-  for (; w + U <= it.ways; w += U) take(std::integral_constant<int, U>{}, w);
-  if (w + 4 <= it.ways) take(std::integral_constant<int, 4>{}, w), w += 4;
-  if (w + 2 <= it.ways) take(std::integral_constant<int, 2>{}, w), w += 2;
-  if (w < it.ways) take(std::integral_constant<int, 1>{}, w);
-  const int cp = pl.by_group.div(col);
-  const int64_t row = (int64_t)it.c.row0 + p0 + cp;
-  const int head = g * a.group + col - cp * a.group;
-  const float inv = inverse_sum(l);
-  T* out = (T*)a.out + (row * a.hq + head) * D + 4 * (lane & 15);
+        for (int i = 0; i < NB; ++i) o[i] += wt * x[u][i];
+      }
+      m = mx;
+    };
+    int w = 0;
+    for (; w + U <= it.ways; w += U) take(std::integral_constant<int, U>{}, w);
+    if (w + 4 <= it.ways) take(std::integral_constant<int, 4>{}, w), w += 4;
+    if (w + 2 <= it.ways) take(std::integral_constant<int, 2>{}, w), w += 2;
+    if (w < it.ways) take(std::integral_constant<int, 1>{}, w);
+    const int cp = pl.by_group.div(col);
+    const int64_t row = (int64_t)it.c.row0 + p0 + cp;
+    const int head = g * a.group + col - cp * a.group;
+    const float inv = inverse_sum(l);
+    T* out = (T*)a.out + (row * a.hq + head) * D + 4 * (lane & 15);
 #pragma unroll
-  for (int i = 0; i < NB; ++i) store4(out + 64 * i, o[i], inv);
-  if (a.lse != nullptr && (lane & 15) == 0) a.lse[(int64_t)head * a.n + row] = log_partition(m, l);
+    for (int i = 0; i < NB; ++i) store4(out + 64 * i, o[i], inv);
+    if (a.lse != nullptr && (lane & 15) == 0) a.lse[(int64_t)head * a.n + row] = log_partition(m, l);
+  }
 }
 
+// (At most some 2048 workgroups: a call that cuts nothing still has them look; 8768 took 15 us.)
 template <typename T, int D, int COLS>
 hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_merge_kernel<T, D, COLS>),
-                     dim3((unsigned)(a.plan.cut_tiles() * a.hkv), COLS / 16), dim3(256), 0, stream, a);
+  const int tiles = a.plan.cut_tiles() * a.hkv;
+  const int runs = 2048 / tiles < 1 ? 1 : 2048 / tiles > COLS / 16 ? COLS / 16 : 2048 / tiles;
+  hipLaunchKernelGGL((paged_merge_kernel<T, D, COLS>), dim3((unsigned)tiles, (unsigned)runs), dim3(256), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
