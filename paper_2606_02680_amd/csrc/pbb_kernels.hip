@@ -524,6 +524,42 @@ void decode_f32_mfma_kernel(DecodeArgs a) {
 // 256-byte rows and 2 ((r >> 1) mod 4) for 128-byte rows: both the 16-byte row reads of the
 // scores and the transposed reads of the values hit distinct banks within every group of lanes
 // that gfx950 serves per cycle.
+// Device-coherent store and load of two floats (8 bytes, aligned; agent scope): they bypass the caches that are not
+// coherent across the chip's compute dies, without writing back or invalidating those caches.
+//
+// Ordering of the split merge.  The partial states are published and read ONLY through these
+// agent-scope atomic accesses, and the unit counter is an agent-scope atomic add; the argument
+// rests on how the AMDGPU backend's memory model for gfx942/gfx950 lowers them (LLVM
+// AMDGPUUsage, "Memory Model GFX942"):
+//   * an agent-scope atomic store or load is a global store/load with sc1 set: the store is
+//     written through this die's L2 to the agent's coherence point, and the load is not served
+//     from a stale line of a non-coherent cache;
+//   * s_waitcnt vmcnt(0) returns only once every earlier store of the wave has been
+//     acknowledged, i.e. is visible at that coherence point.  This is the completion step of
+//     the backend's agent-scope release sequence; the other step of that sequence, the L2
+//     write-back (buffer_wbl2 sc1), exists for stores made WITHOUT sc1, and no partial state is
+//     written that way;
+//   * the acquire sequence's L2 invalidation (buffer_inv sc1) likewise exists for later loads
+//     made without sc1, and the merge reads the workspace only with sc1 loads, which it issues
+//     after the counter's returned value has been observed (the flag goes through LDS and a
+//     workgroup barrier, so no load can be performed before the add has returned).
+// Hence: every store of a workgroup completes (vmcnt(0), then the barrier) before its count is
+// added, and the last arriver's loads read the coherence point after the final count -- the
+// guarantees a release add / acquire load pair would give, without the cache-wide write-back
+// and invalidation (measured 3x slower, because the invalidation also evicts rings that stay
+// cache-resident at small batch).  Relaxed accesses do not carry this guarantee in the
+// language-level model; it is a property of the lowering above, and the graph-replay split
+// tests exercise it every replay.
+__device__ __forceinline__ void coherent_store2(float* p, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32);
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 coherent_load2(const float* p) {
+  const uint64_t v = __hip_atomic_load((uint64_t*)const_cast<float*>(p), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
 template <int D, int NW, bool NT, bool ROPE, bool SPLIT, bool WR>
 __global__ __launch_bounds__(NW * 64) void decode_bf16_kernel(DecodeArgs a) {
   static_assert(!(WR && SPLIT), "whole-ring launches are not split");

@@ -9,7 +9,7 @@
 #include <cmath>
 #include <cstdint>
 
-#include "pbb_internal.h"
+#include "pbb_paged_internal.h"
 
 namespace {
 

@@ -5,9 +5,44 @@
 #include <type_traits>
 
 #include "pbb_device.h"
-#include "pbb_internal.h"
+#include "pbb_paged_internal.h"
 
 namespace pbb {
+
+// read_chunks and wait_chunks of a 16-row tile: dst[nb] holds rows 4j4 .. +3 of channel 16nb + c16.
+template <int D>
+__device__ __forceinline__ void read_tile(u32x2 (&dst)[D / 16], const uint32_t (&ta)[4], uint32_t sb) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) dst[x] = tr_read<0>(ta[x] + sb);
+  if constexpr (D == 128) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) dst[4 + x] = tr_read<kTileLine>(ta[x] + sb);
+  }
+}
+template <int D>
+__device__ __forceinline__ void wait_tile(u32x2 (&v)[D / 16]) {
+  if constexpr (D == 128)
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]),
+                   "+v"(v[6]), "+v"(v[7]));
+  else
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+}
+
+// Device-coherent store and load of two floats (8 bytes, aligned): agent-scope atomics, which on this
+// chip go through to and come from the point where its compute dies meet, past their own caches.  A
+// state published with these stores is complete for whoever reads it with these loads after a counter
+// that was added to once the stores had been acknowledged (s_waitcnt vmcnt(0), then a barrier, then the
+// add): the split decode steps merge by the same protocol, and their kernel says why it holds.
+__device__ __forceinline__ void coherent_store2(float* p, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32);
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 coherent_load2(const float* p) {
+  const uint64_t v = __hip_atomic_load((uint64_t*)const_cast<float*>(p), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
 
 // Inclusive sums over the lanes of a wave (row shifts by 1, 2, 4, 8, then the sums of the rows
 // before: on the VALU).

@@ -11,7 +11,7 @@
 // all rows of the token that it visits.
 
 #include "pbb_device.h"
-#include "pbb_internal.h"
+#include "pbb_paged_internal.h"
 
 namespace pbb {
 namespace {
