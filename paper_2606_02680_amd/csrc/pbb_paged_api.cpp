@@ -82,18 +82,22 @@ pbb::PagedPlan plan_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s, int3
                               d->batch, d->n_kv_heads, group, n, ragged);
 }
 
-// What any call may need, of few columns per sequence or of many (which of them a call is, its
-// q_start decides).
+size_t states_of(const pbb_paged_desc_t* d, const pbb::PagedPlan& p) {
+  return (size_t)p.slots * d->n_kv_heads * pbb::paged_state_bytes(p.cols, d->head_dim);
+}
+
+// What any call may need: calls of few columns per sequence are all planned alike, of the others one of
+// a single token needs most (which of them a call is, its q_start decides).
 size_t workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
   const int group = d->n_q_heads / d->n_kv_heads;
-  size_t bytes = 0;
-  for (const bool narrow : {false, true}) {
-    const pbb::PagedKind k = pbb::paged_kind(d->dtype == PBB_DTYPE_F32, narrow, d->head_dim);
-    const pbb::PagedPlan p = pbb::PagedPlan::make(s, k, d->batch, d->n_kv_heads, group, d->batch, true);
-    const size_t need =
-        (size_t)p.slots * d->n_kv_heads * pbb::paged_state_bytes(k.cols, d->head_dim);
-    bytes = need > bytes ? need : bytes;
-  }
+  const bool f32 = d->dtype == PBB_DTYPE_F32;
+  const size_t narrow = states_of(
+      d, pbb::PagedPlan::make(s, pbb::paged_kind(f32, true, d->head_dim), d->batch, d->n_kv_heads, group,
+                              d->batch, false));
+  const size_t wide = states_of(
+      d, pbb::PagedPlan::make(s, pbb::paged_kind(f32, false, d->head_dim), d->batch, d->n_kv_heads, group,
+                              1, true));
+  const size_t bytes = narrow > wide ? narrow : wide;
   return bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;
 }
 
@@ -241,6 +245,8 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   const size_t need = workspace_of(desc, a.shape);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
+  const size_t states = states_of(desc, a.plan);
+  if (states > 0 && states + pbb::kPagedCounterBytes > need) return PBB_ERR_WORKSPACE;  // (never)
   if ((uint64_t)a.plan.items() * (uint64_t)desc->n_kv_heads > 0x7fffffffull) return PBB_ERR_SHAPE;
   a.counters = need > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
   a.states = need > 0 ? reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) +

@@ -134,11 +134,14 @@ struct PagedPlan {
                      : batch * ((p.uniform + p.tq - 1) / p.tq);
     const int all = k.round / hkv, many = k.pieces / hkv;
     const int round = all - (p.tiles < all / 2 ? p.tiles : all / 2);
-    p.few_least = round > 0 ? k.few_least : k.many_least;
+    p.few_least = round > 0 && k.few_least < k.many_least ? k.few_least : k.many_least;
     p.many_least = k.many_least;
     p.per_round = 1.0f / (float)(round > 0 ? round : 1);
     p.per_pieces = 1.0f / (float)(many > 0 ? many : 1);
-    p.pieces = longest_walk(s, k, p.tq) > p.few_least && 2 * hkv <= kPagedMaxPieces
+    // (Walks of fewer than many_least steps are worth the merge launch only where there are few: 512
+    // tokens of four prompts, 32/8 heads, 28.5 us, 33.2 with a launch that finds nothing to merge.)
+    const int worth = !p.narrow && 4 * p.tiles >= all ? k.many_least : p.few_least;
+    p.pieces = longest_walk(s, k, p.tq) > worth && 2 * hkv <= kPagedMaxPieces
                    ? (round > many ? round : many) : 0;
     p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
     return p;

@@ -92,10 +92,11 @@ inline PagedKind paged_kind(bool f32, bool narrow, int head_dim) {
   // heads: 125 / 134 with 64).
   if (f32 && narrow) return PagedKind{kPagedNarrowCols, kPagedStepF32, 512, 8, 2048, 32};
   if (narrow) return PagedKind{kPagedNarrowCols, kPagedStep, head_dim == 64 ? 512 : 256, 8, 2048, 64};
-  // Many columns: states are large, pieces of fewer than 32 steps cost more than they gain (512 tokens
-  // of four prompts 28.7 us, 50 with 16; 128 tokens behind 16000 57, 69 with 64 steps).
-  if (f32) return PagedKind{kPagedColsF32, kPagedStepF32, 0, 0, 2048, 32};
-  return PagedKind{kPagedCols, kPagedStep, 0, 0, 1024, 32};
+  // Many columns: two workgroups per CU are a round, and shares of 32 steps and more come under the
+  // second rule, since states are large (one sequence of 26 tokens behind 9900, 16/2 heads: 25.7 us, 38.5
+  // with pieces of 32 steps; 128 tokens behind 16000, 32/8 heads: 57 with 32, 69 with 64).
+  if (f32) return PagedKind{kPagedColsF32, kPagedStepF32, 512, 8, 2048, 32};
+  return PagedKind{kPagedCols, kPagedStep, 512, 8, 1024, 32};
 }
 constexpr size_t kPagedCounterBytes = 65536;
 

@@ -213,6 +213,11 @@ int main() {
     const PagedKind kind_of{narrow ? 16 : f32 ? 64 : 128, f32 ? 16 : 32, pick(0, 3) ? pick(1, 1024) : 0,
                             pick(1, 40), pick(1, kPagedMaxPieces), pick(1, 80)};
     const PagedPlan p = PagedPlan::make(s, kind_of, batch, hkv, group, n, ragged);
+    // the workspace, sized for one token (for calls of few columns: for the call itself), is enough
+    if (!narrow && p.slots > PagedPlan::make(s, kind_of, batch, hkv, group, 1, true).slots)
+      return std::printf("workspace %d\n", i), 1;
+    if (narrow && p.slots != PagedPlan::make(s, kind_of, batch, hkv, group, batch, false).slots)
+      return std::printf("workspace of few columns %d\n", i), 1;
     if (p.narrow != narrow || (narrow && per > p.tq)) return std::printf("narrow %d\n", i), 1;
     if ((p.tq < 1) || (int64_t)p.slots * hkv * 4 > 65536) return std::printf("slots %d\n", i), 1;
     float total = 0;
