@@ -93,14 +93,25 @@ struct PagedItem {
 template <bool CUT>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane, PagedItem& it) {
   const PagedPlan& p = a.plan;
+  if (!CUT && p.uniform >= 0 && p.pieces == 0) {   // nothing to search for
+    const int tiles = p.tiles_of(Chunk{0, p.uniform, 0});
+    it.b = tiles == 1 ? item : item / tiles;
+    if (it.b >= a.batch) return false;
+    it.tile = tiles - 1 - (item - it.b * tiles);
+    it.piece = 0;
+    it.ways = 1;
+    it.slot = 0;
+    it.c = chunk_of(it.b, p.uniform, 0, 0, scalar_word(a.pos, (size_t)it.b), a.n);
+    return true;
+  }
   auto chunk = [&](int b) -> Chunk {
     if (b >= a.batch) return Chunk{0, 0, 0};
     const bool ragged = p.uniform < 0;
     return chunk_of(b, p.uniform, ragged ? a.q_start[b] : 0, ragged ? a.q_start[b + 1] : 0, a.pos[b],
                     a.n);
   };
-  // the first 256 sequences' chunks, their loads in flight together
-  constexpr int KEPT = 4;
+  // the first 128 sequences' chunks, their loads in flight together
+  constexpr int KEPT = 2;
   Chunk kept[KEPT];
 #pragma unroll
   for (int r = 0; r < KEPT; ++r) kept[r] = chunk(64 * r + lane);
@@ -113,7 +124,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     for (int b0 = 64 * KEPT; b0 < a.batch; b0 += 64)
       if (!visit(b0, chunk(b0 + lane))) return;
   };
-  float share = 1.0e30f;
+  float per_share = 0.0f;
   if (p.pieces > 0) {
     float sum = 0.0f;
     uint32_t count = 0;
@@ -128,14 +139,14 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     const uint32_t tiles = (uint32_t)lane_value((int)wave_scan(count), 63);
     // (q_start entries out of order can name more tiles than the launch has room for: no walk is
     // cut then, so that no merge waits for a piece that does not run)
-    if (tiles <= (uint32_t)p.tiles) share = p.share_of(total);
+    if (tiles <= (uint32_t)p.tiles) per_share = 1.0f / p.share_of(total);
   }
   uint32_t base = 0, sbase = 0;
   bool found = false;
   auto search = [&](auto&& mine) {   // among the sequences that mine(tokens) takes
     round([&](int b0, const Chunk& c) {
       const int nt = mine(c.count) ? p.tiles_of(c) : 0;
-      const int ways = p.pieces_of(p.steps_of(a.shape, c), share);
+      const int ways = p.pieces_of(p.steps_of(a.shape, c), per_share);
       const uint32_t pieces = (uint32_t)nt * (uint32_t)ways;
       const uint32_t cut = ways > 1 ? pieces : 0u;
       const uint32_t count = !CUT ? pieces : ways > 1 ? (uint32_t)nt : 0u;

@@ -64,12 +64,10 @@ struct PagedShape {
   // A table entry, made safe to address with: 0 in place of one that names no page.
   PBB_HD bool is_page(int id) const { return (uint32_t)id < (uint32_t)n_pages; }
   // Keys that a run of `tokens` targets ending at position `last` can walk, at most.
-  PBB_HD int64_t max_keys(int last, int tokens) const {
-    const int64_t all = (int64_t)(last < capacity ? last + 1 : capacity);
-    const int64_t span = support == kPagedPBB   ? 2 * (int64_t)half + tokens
-                         : support == kPagedSWA ? (int64_t)window + tokens
-                                                : all;
-    return span < all ? span : all;
+  PBB_HD uint32_t max_keys(int last, int tokens) const {
+    const uint32_t all = (uint32_t)(last < capacity ? last + 1 : capacity);
+    const uint32_t span = (support == kPagedPBB ? 2u * (uint32_t)half : (uint32_t)window) + (uint32_t)tokens;
+    return support != kPagedFull && span < all ? span : all;
   }
 };
 
@@ -96,7 +94,7 @@ constexpr int kPagedMaxPieces = 2048;   // budget of a call's KV heads together,
 // none so short that its first loads and its merge cost more than that gains.
 struct PagedKind {
   int cols;     // query columns of a tile
-  int step;     // keys per step
+  int step;     // keys per step, 16 or 32
   int round;    // workgroups of one round, in all heads (0: always the second rule)
   int few_least;
   int pieces;   // in all heads
@@ -106,7 +104,7 @@ struct PagedKind {
 struct PagedPlan {
   int cols;      // query columns of a tile
   int tq;        // tokens per tile
-  int step;      // keys per step
+  int step, step_bits;   // keys per step, a power of two
   int pieces;    // pieces of cut walks per KV head, at most; 0: no walk is cut
   int few_least, many_least;
   float per_round, per_pieces;   // 1 / workgroups of a round, 1 / pieces, per KV head
@@ -126,6 +124,7 @@ struct PagedPlan {
     p.cols = k.cols;
     p.tq = p.cols / group;
     p.step = k.step;
+    p.step_bits = k.step == 16 ? 4 : 5;
     p.by_hkv = FastDiv::make((uint32_t)hkv);
     p.by_tq = FastDiv::make((uint32_t)p.tq);
     p.by_group = FastDiv::make((uint32_t)group);
@@ -140,26 +139,29 @@ struct PagedPlan {
     p.per_pieces = 1.0f / (float)(many > 0 ? many : 1);
     // (Walks of fewer than many_least steps are worth the merge launch only where there are few: 512
     // tokens of four prompts, 32/8 heads, 28.5 us, 33.2 with a launch that finds nothing to merge.)
-    const int worth = !p.narrow && 4 * p.tiles >= all ? k.many_least : p.few_least;
+    // Single tokens merge without one: there it is the search for a workgroup's item that a call without
+    // cut walks is spared (293 of at most 30 keys, 32/8 heads, fp32: 58.5 us, 28.7 without it).
+    const bool many_tiles = p.narrow ? p.tiles >= 4 * all : 4 * p.tiles >= all;
+    const int worth = many_tiles ? k.many_least : p.few_least;
     p.pieces = longest_walk(s, k, p.tq) > worth && 2 * hkv <= kPagedMaxPieces
                    ? (round > many ? round : many) : 0;
     p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
     return p;
   }
   static int64_t longest_walk(const PagedShape& s, const PagedKind& k, int tq) {
-    return (s.max_keys(s.capacity, tq) + k.step - 1) / k.step + 1;
+    return (int64_t)((s.max_keys(s.capacity, tq) + k.step - 1) / k.step) + 1;
   }
   // Tiles of a chunk, and the longest walk of one of them in steps.
   PBB_HD int tiles_of(const Chunk& c) const { return c.count > 0 ? by_tq.div(c.count - 1) + 1 : 0; }
   PBB_HD int steps_of(const PagedShape& s, const Chunk& c) const {
     if (c.pos < 0 || c.count == 0) return 1;
-    const int64_t keys = s.max_keys(c.pos + c.count - 1, tq < c.count ? tq : c.count);
-    return (int)((keys + step - 1) / step) + 1;
+    const uint32_t keys = s.max_keys(c.pos + c.count - 1, tq < c.count ? tq : c.count);
+    return (int)((keys + (1u << step_bits) - 1) >> step_bits) + 1;
   }
-  // Pieces of each of a sequence's walks, share = the steps C of a piece.
-  PBB_HD int pieces_of(int steps, float share) const {
+  // Pieces of each of a sequence's walks, per_share = 1 / C (C the steps of a piece).
+  PBB_HD int pieces_of(int steps, float per_share) const {
     if (pieces == 0) return 1;
-    const int p = (int)__builtin_ceilf((float)steps / share);
+    const int p = (int)__builtin_ceilf((float)steps * per_share);
     return p > 1 ? p : 1;
   }
   PBB_HD float share_of(float total) const {

@@ -322,7 +322,7 @@ def test_attention_chunks(cuda, dtype, lens, d, hq, hkv, page, block, window):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_many_sequences(cuda, dtype):
-    """More sequences than a wave keeps in registers (256): single tokens, one long walk among them, and
+    """More sequences than a wave keeps in registers (128): single tokens, one long walk among them, and
     a ragged mixture with skipped and empty sequences."""
     lens = [((i * 13) % 40, 1) for i in range(699)] + [(1200, 1)]
     _check(Cache(lens, 2, 1, 64, 16, dtype, seed=15, uniform=True, fill=math.nan), cuda)

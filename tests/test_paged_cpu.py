@@ -231,7 +231,7 @@ int main() {
     const float share = p.share_of(total);
     int64_t items = 0, slots = 0;
     for (auto& c : cs) {
-      const int steps = p.steps_of(s, c), ways = p.pieces_of(steps, share);
+      const int steps = p.steps_of(s, c), ways = p.pieces_of(steps, 1.0f / share);
       items += (int64_t)p.tiles_of(c) * ways;
       if (ways > 1) slots += (int64_t)p.tiles_of(c) * ways, ++cut;
       // no tile walks more steps than the plan counts
