@@ -220,7 +220,8 @@ pbb_status_t pbb_decode_step_noalloc(const pbb_desc_t *desc, const int32_t *pos,
  * 0 <= n <= 2^30 and n_q_heads * head_dim <= 2^24 (PBB_ERR_SHAPE otherwise); n == 0 does
  * nothing.  q, k, v, out, rings 16-byte aligned, lse 4-byte
  * aligned.  Same descriptor rules as pbb_decode_step, and rope_base must be 0 (rotate q and k
- * before the call; the ring then holds rotated keys as a rotary decode expects); no workspace.
+ * before the call, see pbb_rotate; the ring then holds rotated keys as a rotary decode expects); no
+ * workspace.
  */
 pbb_status_t pbb_prefill(const pbb_desc_t *desc, int32_t n, const void *q, const void *k,
                          const void *v, void *out, float *lse, void *k_ring, void *v_ring,
@@ -327,7 +328,7 @@ pbb_status_t pbb_rotate(const pbb_rope_t *rope, int32_t n_tokens, int32_t n_head
  * become zero, lse -inf, nothing is appended.
  *
  * Constraints (PBB_ERR_SHAPE otherwise): batch >= 1; heads and head_dim as pbb_desc_t; page_size a
- * multiple of 16; n_pages >= 1; table_width >= 1; table_width * page_size <= 2^30;
+ * multiple of 16, at most 2^20; n_pages >= 1; table_width >= 1; table_width * page_size <= 2^30;
  * n_q_heads * head_dim <= 2^24; 0 <= n_tokens <= 2^30; block even, window and block >= 0 and not
  * both set; batch * table_width, and n_q_heads * n_tokens, below 2^40.
  */

@@ -20,6 +20,7 @@ static_assert((2 * pbb::kPagedMaxPieces + pbb::kPagedMaxPieces / 8 + pbb::kPaged
 
 constexpr int32_t kMaxTokens = 1 << 30;
 constexpr int32_t kMaxCapacity = 1 << 30;
+constexpr int32_t kMaxPage = 1 << 20;   // (a page's rows under one KV head lie within 32-bit byte offsets)
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -59,8 +60,8 @@ pbb_status_t check_paged(const pbb_paged_desc_t* d, int32_t n) {
   if (d->n_q_heads / d->n_kv_heads > pbb::kMaxGroup) return PBB_ERR_SHAPE;
   if (d->head_dim != 64 && d->head_dim != 128) return PBB_ERR_SHAPE;
   if ((int64_t)d->n_q_heads * d->head_dim > (1 << 24)) return PBB_ERR_SHAPE;
-  if (d->page_size < 16 || d->page_size % 16 != 0 || d->n_pages < 1 || d->table_width < 1)
-    return PBB_ERR_SHAPE;
+  if (d->page_size < 16 || d->page_size > kMaxPage || d->page_size % 16 != 0) return PBB_ERR_SHAPE;
+  if (d->n_pages < 1 || d->table_width < 1) return PBB_ERR_SHAPE;
   if ((int64_t)d->page_size * d->table_width > kMaxCapacity) return PBB_ERR_SHAPE;
   if (d->block < 0 || d->block % 2 != 0 || d->window < 0 || (d->block > 0 && d->window > 0))
     return PBB_ERR_SHAPE;

@@ -312,6 +312,14 @@ def test_attention_column_limits(cuda, dtype, d, hq, hkv, page, lens, ragged):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_one_page_per_sequence(cuda, dtype):
+    """Pages of 65536 rows, as a cache without paging has them."""
+    c = Cache([(70, 50), (0, 1), (333, 2)], 4, 1, 64, 65536, dtype, seed=21, fill=math.nan)
+    _check(c, cuda)
+    _check(c, cuda, block=100)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("lens", [[(1000, 100)], [(0, 300)], [(513, 150), (3, 1), (640, 1), (20, 40)]])
 @pytest.mark.parametrize("d,hq,hkv,page,block,window", [(128, 4, 1, 16, 0, 0), (64, 6, 2, 48, 0, 0),
                                                         (128, 3, 1, 64, 256, 0), (64, 8, 1, 16, 0, 333)])

@@ -102,6 +102,7 @@ def test_rotate_refusals():
 
 BAD_SHAPES = [dict(batch=0), dict(n_kv_heads=0), dict(n_q_heads=0), dict(n_q_heads=7), dict(n_q_heads=34),
               dict(head_dim=96), dict(page_size=0), dict(page_size=8), dict(page_size=24),
+              dict(page_size=(1 << 20) + 16),
               dict(n_pages=0), dict(table_width=0), dict(page_size=1 << 20, table_width=1 << 12),
               dict(block=-2), dict(block=7), dict(window=-1), dict(block=64, window=64)]
 
