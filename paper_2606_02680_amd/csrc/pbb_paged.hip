@@ -9,8 +9,14 @@
 // loaded once per workgroup: wave w loads 16 rows of K or V, which lie in one page, so a step costs a
 // wave one table entry, read through the scalar cache a step ahead.  S^T = K Q^T and O^T += V^T P^T on
 // v_mfma_f32_16x16x32_bf16, with an online softmax whose reference moves lazily, as in the prefill.
-// Long walks are cut into pieces (PagedPlan), which leave partial states (Eq.(lse)) that the last of
-// them to end merges.
+// Long walks are cut into pieces (PagedPlan), which leave partial states (Eq.(lse)); a second launch
+// merges those of wide tiles, the last piece to end those of single tokens.  Sequences of few columns go
+// through narrow_walk, in the same launch.
+//
+// Bound: with many columns the matrix and vector work of a step at the clock that the card's power
+// allows (16384 tokens, 32/8 heads, d 128: 1872 to 1965 us over the boxes measured, 1120 to 1175
+// TFLOP/s, matrix cores 0.52 busy at 1.97 GHz); with few columns HBM (192 single tokens at up to 32768:
+// 1865 us, 6.7 TB/s).
 //
 // Masks.  Steps with a key outside some column's support set its scores to -inf.  What such keys hold
 // is unknown (rows never written, dropped pages), and 0 * inf or 0 * NaN would reach the products, so
@@ -60,7 +66,8 @@ __device__ __forceinline__ uint32_t special_halves(uint32_t w) {
 // merge of the waves at the end waits for another wave.  A wave has three 16-row tiles: while it works
 // on one, the two after it (K and V rows alternate) are in flight; a tile is loaded over as soon as it
 // has been read.  The value products contract 16 keys (v_mfma_f32_16x16x16_bf16).
-// Bound: HBM, with 12 waves per CU, 8 KiB of each in flight.
+// Bound: HBM, with 12 waves per CU, 8 KiB of each in flight.  (32-key steps with two buffers per wave
+// take 64 KiB for two waves: 256 single tokens of up to 600 71 us, 67 so.)
 template <int D>
 constexpr int narrow_lds() { return kPagedWaves * 3 * 16 * D * 2; }
 
@@ -386,7 +393,7 @@ void paged_bf16_kernel(PagedArgs a) {
   const int g = (int)blockIdx.x - item * a.hkv;
   PagedItem it;
   if (!find_item<false>(a, item, lane, it)) return;
-  if (it.c.count * G <= kPagedNarrowCols) {
+  if (it.c.count <= pl.narrow_tokens) {
     static_assert(narrow_lds<D>() <= STAGES * BUF, "LDS");
     narrow_walk<D, false>(a, it, g, smem);
     return;

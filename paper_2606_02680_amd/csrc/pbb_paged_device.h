@@ -175,8 +175,8 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
   if (p.uniform >= 0) {
     search([](int) { return true; });
   } else {
-    search([&](int count) { return count * a.group > kPagedNarrowCols; });
-    if (!found) search([&](int count) { return count * a.group <= kPagedNarrowCols; });
+    search([&](int count) { return count > p.narrow_tokens; });
+    if (!found) search([&](int count) { return count <= p.narrow_tokens; });
   }
   return found;
 }

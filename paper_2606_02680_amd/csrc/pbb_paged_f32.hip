@@ -334,7 +334,7 @@ void paged_f32_kernel(PagedArgs a) {
   const int g = (int)blockIdx.x - item * a.hkv;
   PagedItem it;
   if (!find_item<false>(a, item, lane, it)) return;
-  if (it.c.count * G <= kPagedNarrowCols) {
+  if (it.c.count <= pl.narrow_tokens) {
     static_assert(sizeof(smem) >= kF32Waves * kPagedNarrowCols * (D + 2) * 4, "LDS");
     narrow_walk_f32<D, false>(a, it, g, smem);
     return;

@@ -110,6 +110,7 @@ struct PagedPlan {
   float per_round, per_pieces;   // 1 / workgroups of a round, 1 / pieces, per KV head
   int uniform;   // tokens of every sequence, -1: q_start says
   int narrow;    // 1: at most kPagedNarrowCols columns per sequence
+  int narrow_tokens;   // tokens of that many columns
   int tiles;     // tiles of a call, at most
   int slots;     // partial states per KV head, at most
   FastDiv by_hkv, by_tq, by_group;
@@ -121,6 +122,7 @@ struct PagedPlan {
     PagedPlan p;
     p.uniform = ragged ? -1 : n_tokens / batch;
     p.narrow = is_narrow(batch, group, n_tokens, ragged);
+    p.narrow_tokens = kPagedNarrowCols / group;
     p.cols = k.cols;
     p.tq = p.cols / group;
     p.step = k.step;
