@@ -300,8 +300,9 @@ pbb_status_t pbb_rope_init(pbb_rope_t *rope, int32_t head_dim, double base, int3
  *   positions  int32 [n_axes][n_tokens], any value (negative ones turn backwards)
  * Angles are reduced to a turn in fp64.  float32: fp32 sines and cosines of the reduced angle;
  * bfloat16: fp32 arithmetic, rounded RNE once.  out may be x itself (with the same stride); other
- * overlaps are undefined.  0 <= n_tokens <= 2^30 (0 does nothing), 1 <= n_heads,
- * n_heads * head_dim <= 2^24 (PBB_ERR_SHAPE otherwise).  x, out 16-byte aligned, positions 4-byte.
+ * overlaps are undefined.  0 <= n_tokens <= 2^30 (0 does nothing, and its tensors may be NULL),
+ * 1 <= n_heads, n_heads * head_dim <= 2^24 (PBB_ERR_SHAPE otherwise).  x, out 16-byte aligned,
+ * positions 4-byte.
  */
 pbb_status_t pbb_rotate(const pbb_rope_t *rope, int32_t n_tokens, int32_t n_heads,
                         const int32_t *positions, const void *x, int64_t x_stride, void *out,
@@ -329,8 +330,9 @@ pbb_status_t pbb_rotate(const pbb_rope_t *rope, int32_t n_tokens, int32_t n_head
  *
  * Constraints (PBB_ERR_SHAPE otherwise): batch >= 1; heads and head_dim as pbb_desc_t; page_size a
  * multiple of 16, at most 2^20; n_pages >= 1; table_width >= 1; table_width * page_size <= 2^30;
- * n_q_heads * head_dim <= 2^24; 0 <= n_tokens <= 2^30; block even, window and block >= 0 and not
- * both set; batch * table_width, and n_q_heads * n_tokens, below 2^40.
+ * n_q_heads * head_dim <= 2^24; 0 <= n_tokens <= 2^30 (0 does nothing, and its tensors may be NULL);
+ * block even, window and block >= 0 and not both set; batch * table_width, and n_q_heads *
+ * n_tokens, below 2^40.
  */
 typedef struct {
   int32_t batch;

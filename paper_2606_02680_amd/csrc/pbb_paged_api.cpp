@@ -141,10 +141,10 @@ pbb_status_t pbb_rotate(const pbb_rope_t* rope, int32_t n_tokens, int32_t n_head
   if (!stride_ok(x_stride, n_heads, rope->head_dim, u) ||
       !stride_ok(out_stride, n_heads, rope->head_dim, u))
     return PBB_ERR_SHAPE;
+  if (n_tokens == 0) return PBB_OK;   // (tensors of no tokens may have no address)
   if (out == x && out_stride != x_stride) return PBB_ERR_SHAPE;
   if (!positions || !x || !out) return PBB_ERR_NULL;
   if (!aligned(positions, 4) || !aligned(x, 16) || !aligned(out, 16)) return PBB_ERR_ALIGN;
-  if (n_tokens == 0) return PBB_OK;
   pbb::RotateArgs a;
   a.x = x;
   a.out = out;
@@ -178,6 +178,7 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t* desc, int32_t n_tokens, co
       !stride_ok(v_stride, desc->n_kv_heads, desc->head_dim, u) ||
       (q != nullptr && !stride_ok(q_stride, desc->n_q_heads, desc->head_dim, u)))
     return PBB_ERR_SHAPE;
+  if (n_tokens == 0) return PBB_OK;
   if (q != nullptr && q_out == q && q_stride != (int64_t)desc->n_q_heads * desc->head_dim)
     return PBB_ERR_SHAPE;
   if (!pos || !table || !k || !v || !k_pages || !v_pages) return PBB_ERR_NULL;
@@ -186,7 +187,6 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t* desc, int32_t n_tokens, co
       !aligned(q, 16) || !aligned(q_out, 16) || !aligned(k, 16) || !aligned(v, 16) ||
       !aligned(k_pages, 16) || !aligned(v_pages, 16))
     return PBB_ERR_ALIGN;
-  if (n_tokens == 0) return PBB_OK;
   pbb::AppendArgs a;
   a.pos = pos;
   a.q_start = q_start;
@@ -234,11 +234,11 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   if (q_start == nullptr && n_tokens % desc->batch != 0) return PBB_ERR_SHAPE;
   const int64_t u = elem_bytes(desc->dtype);
   if (!stride_ok(q_stride, desc->n_q_heads, desc->head_dim, u)) return PBB_ERR_SHAPE;
+  if (n_tokens == 0) return PBB_OK;
   if (!pos || !table || !q || !k_pages || !v_pages || !out) return PBB_ERR_NULL;
   if (!aligned(pos, 4) || !aligned(q_start, 4) || !aligned(table, 4) || !aligned(q, 16) ||
       !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) || !aligned(lse, 4))
     return PBB_ERR_ALIGN;
-  if (n_tokens == 0) return PBB_OK;
 
   pbb::PagedArgs a;
   a.shape = shape_of(desc);

@@ -581,7 +581,7 @@ def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out
     if workspace is not None:
         _expect_on("workspace", workspace, dev)
         ws_bytes = workspace.numel() * workspace.element_size()
-    elif paged_workspace_bytes(desc, n) > 0:
+    elif n > 0 and paged_workspace_bytes(desc, n) > 0:
         workspace = _scratch_on(stream, lambda: alloc_paged_workspace(desc, n, q.device))
         ws_bytes = workspace.numel()
     status = load_library().pbb_paged_attention(

@@ -664,3 +664,21 @@ def test_binding_refusals(cuda):
         wide = torch.empty(4, 66, device=cuda, dtype=BF)
         P.pbb_rotate(P.make_rope(64, BASE), torch.zeros(4, device=cuda, dtype=torch.int32),
                      wide[:, :64].unsqueeze(1), torch.empty(4, 1, 64, device=cuda, dtype=BF))
+
+
+def test_no_tokens(cuda):
+    """A step that brings nothing."""
+    desc = P.make_paged_desc(2, 4, 2, 64, page_size=16, n_pages=3, table_width=2)
+    pages = P.alloc_pages(desc)
+    before = [bits(t).cpu() for t in pages]
+    pos = torch.zeros(2, dtype=torch.int32, device=cuda)
+    table = torch.zeros(2, 2, dtype=torch.int32, device=cuda)
+    q_start = torch.zeros(3, dtype=torch.int32, device=cuda)
+    q, kv = (torch.empty(0, h, 64, dtype=BF, device=cuda) for h in (4, 2))
+    P.pbb_rotate(P.make_rope(64, BASE), torch.empty(0, dtype=torch.int32, device=cuda), q, q)
+    for start in (None, q_start):
+        P.pbb_paged_append(desc, pos, table, kv, kv, *pages, q_start=start, rope=P.make_rope(64, BASE), q=q,
+                           q_out=q)
+        P.pbb_paged_attention(desc, pos, table, q, *pages, torch.empty_like(q), q_start=start)
+    for t, b in zip(pages, before):
+        assert torch.equal(bits(t).cpu(), b)

@@ -266,3 +266,12 @@ def test_index_arithmetic(tmp_path):
     subprocess.run(["g++", "-O1", "-std=c++17", "-I", inc, str(src), "-o", exe], check=True)
     p = subprocess.run([exe], capture_output=True, text=True)
     assert p.returncode == 0, p.stdout
+
+
+def test_no_tokens():
+    """Calls of no tokens do nothing; their tensors have no address."""
+    assert _rotate(n=0, positions=0, x=0, out=0) == 0
+    assert _append(n=0, k=0, v=0) == 0
+    assert _append(n=0, k=0, v=0, rope=_rope(), pos=0, table=0) == 0
+    assert _attend(n=0, q=0, out=0) == 0
+    assert _rotate(n=0, x=0, out=0, heads=0) == SHAPE and _attend(_desc(batch=0), n=0) == SHAPE
