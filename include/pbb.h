@@ -328,11 +328,13 @@ pbb_status_t pbb_rotate(const pbb_rope_t *rope, int32_t n_tokens, int32_t n_head
  * negative pos[b], or one above 2^31 - 1 - n_tokens, skips the sequence: its rows of q_out and out
  * become zero, lse -inf, nothing is appended.
  *
- * Constraints (PBB_ERR_SHAPE otherwise): batch >= 1; heads and head_dim as pbb_desc_t; page_size a
- * multiple of 16, at most 2^20; n_pages >= 1; table_width >= 1; table_width * page_size <= 2^30;
+ * Constraints (PBB_ERR_SHAPE otherwise): 1 <= batch <= 2^24; heads and head_dim as pbb_desc_t;
+ * page_size a multiple of 16, at most 2^20; n_pages >= 1; table_width >= 1; table_width * page_size <= 2^30;
  * n_q_heads * head_dim <= 2^24; 0 <= n_tokens <= 2^30 (0 does nothing, and its tensors may be NULL);
  * block even, window and block >= 0 and not both set; batch * table_width, and n_q_heads *
- * n_tokens, below 2^40.
+ * n_tokens, below 2^40.  An attention call has at most 2^23 tiles in all KV heads: a sequence's tokens
+ * in runs of floor(T / G), T = 128, float32 64; with q_start, n_tokens / floor(T / G) (rounded down)
+ * and min(batch, n_tokens) more.
  */
 typedef struct {
   int32_t batch;

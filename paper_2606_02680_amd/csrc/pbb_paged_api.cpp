@@ -20,6 +20,10 @@ static_assert((2 * pbb::kPagedMaxPieces + pbb::kPagedMaxPieces / 8 + pbb::kPaged
 
 constexpr int32_t kMaxTokens = 1 << 30;
 constexpr int32_t kMaxCapacity = 1 << 30;
+constexpr int32_t kMaxBatch = 1 << 24;
+// Tiles of an attention call in all heads.  With the pieces (some 2176) and one workgroup per head (at
+// most 2^18) more, a launch of 256 threads each stays below 2^32 threads.
+constexpr uint64_t kMaxTiles = 1u << 23;
 constexpr int32_t kMaxPage = 1 << 20;   // (a page's rows under one KV head lie within 32-bit byte offsets)
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -55,7 +59,7 @@ bool stride_ok(int64_t stride, int64_t heads, int64_t d, int64_t u) {
 pbb_status_t check_paged(const pbb_paged_desc_t* d, int32_t n) {
   if (d == nullptr) return PBB_ERR_NULL;
   if (!known_dtype(d->dtype)) return PBB_ERR_DTYPE;
-  if (d->batch < 1 || d->n_kv_heads < 1 || d->n_q_heads < 1) return PBB_ERR_SHAPE;
+  if (d->batch < 1 || d->batch > kMaxBatch || d->n_kv_heads < 1 || d->n_q_heads < 1) return PBB_ERR_SHAPE;
   if (d->n_q_heads % d->n_kv_heads != 0) return PBB_ERR_SHAPE;
   if (d->n_q_heads / d->n_kv_heads > pbb::kMaxGroup) return PBB_ERR_SHAPE;
   if (d->head_dim != 64 && d->head_dim != 128) return PBB_ERR_SHAPE;
@@ -235,20 +239,19 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   const int64_t u = elem_bytes(desc->dtype);
   if (!stride_ok(q_stride, desc->n_q_heads, desc->head_dim, u)) return PBB_ERR_SHAPE;
   if (n_tokens == 0) return PBB_OK;
+  pbb::PagedArgs a;
+  a.shape = shape_of(desc);
+  a.plan = plan_of(desc, a.shape, n_tokens, q_start != nullptr);
+  if ((uint64_t)a.plan.tiles * (uint64_t)desc->n_kv_heads > kMaxTiles) return PBB_ERR_SHAPE;
   if (!pos || !table || !q || !k_pages || !v_pages || !out) return PBB_ERR_NULL;
   if (!aligned(pos, 4) || !aligned(q_start, 4) || !aligned(table, 4) || !aligned(q, 16) ||
       !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) || !aligned(lse, 4))
     return PBB_ERR_ALIGN;
-
-  pbb::PagedArgs a;
-  a.shape = shape_of(desc);
-  a.plan = plan_of(desc, a.shape, n_tokens, q_start != nullptr);
   const size_t need = workspace_of(desc, a.shape);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
   const size_t states = states_of(desc, a.plan);
   if (states > 0 && states + pbb::kPagedCounterBytes > need) return PBB_ERR_WORKSPACE;  // (never)
-  if ((uint64_t)a.plan.items() * (uint64_t)desc->n_kv_heads > 0x7fffffffull) return PBB_ERR_SHAPE;
   a.counters = need > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
   a.states = need > 0 ? reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) +
                                                  pbb::kPagedCounterBytes)

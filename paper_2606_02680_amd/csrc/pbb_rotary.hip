@@ -17,6 +17,13 @@ namespace pbb {
 namespace {
 
 constexpr int kRotThreads = 256;
+// A grid's x has fewer than 2^32 threads: groups of tokens beyond kGridX go on along z.
+constexpr int kGridX = 1 << 23;
+__device__ __forceinline__ int token_group() { return (int)(blockIdx.z * kGridX + blockIdx.x); }
+dim3 token_grid(int64_t groups, int runs) {
+  return dim3((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)runs,
+              (unsigned)((groups + kGridX - 1) / kGridX));
+}
 // Rows of more bytes than the last-level cache (256 MB) are read and written with the non-temporal
 // hint: what is written first is gone before anything reads it (4 x 16384 tokens of 32 heads, d 128:
 // 537 MB, 259 us with the 8 key heads' call, 235 with the hint, 5.7 TB/s; 16000 tokens, 131 MB: the
@@ -87,7 +94,7 @@ __device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&
   hi = Piece<T>::put(oy);
 }
 
-// Grid: x = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token has
+// Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token has
 // fewer heads than a wave takes rows, a wave takes several tokens (2 heads, d 64, 16000 tokens with 12
 // query heads: 20.9 us for both calls with one token per wave, 15.9 with eight).
 template <typename T, int D, bool NT>
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   const int lane = threadIdx.x & 63;
   const int row = lane / PC;
   const int sub = a.tokens_per_wave > 1 ? a.by_heads.div(row) : 0;   // token within the wave's
-  const int64_t tok = ((int64_t)blockIdx.x * (kRotThreads / 64) + (threadIdx.x >> 6)) * a.tokens_per_wave + sub;
+  const int64_t tok = ((int64_t)token_group() * (kRotThreads / 64) + (threadIdx.x >> 6)) * a.tokens_per_wave + sub;
   if (tok >= a.n || sub >= a.tokens_per_wave) return;
   const int pc = lane % PC;
   float cs[Piece<T>::N], sn[Piece<T>::N];
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(kRotThreads) void paged_append_kernel(AppendArgs a)
   constexpr int ROWB = D * (int)sizeof(T);
   const int lane = threadIdx.x & 63;
   const int tok = __builtin_amdgcn_readfirstlane(
-      (int)(blockIdx.x * (kRotThreads / 64) + (threadIdx.x >> 6)));
+      (int)((uint32_t)token_group() * (kRotThreads / 64) + (threadIdx.x >> 6)));
   if (tok >= a.n) return;
   const int b = a.uniform >= 0 ? a.by_uniform.div(tok) : sequence_of(a.q_start, a.batch, tok, lane);
   if (b < 0) return;
@@ -226,7 +233,7 @@ hipError_t rotate_t(const RotateArgs& a0, hipStream_t stream) {
   a.tokens_per_wave = a.heads < ROWS ? ROWS / a.heads : 1;
   a.run = a.heads < ROWS ? a.heads : head_run(a.n, a.heads, ROWS);
   const int per = WAVES * a.tokens_per_wave;
-  const dim3 grid((unsigned)(((int64_t)a.n + per - 1) / per), (unsigned)((a.heads + a.run - 1) / a.run));
+  const dim3 grid = token_grid(((int64_t)a.n + per - 1) / per, (a.heads + a.run - 1) / a.run);
   const int64_t bytes = (int64_t)a.n * a.heads * D * (int64_t)sizeof(T);
   if (bytes > kStreamBytes)
     hipLaunchKernelGGL((rotate_kernel<T, D, true>), grid, dim3(kRotThreads), 0, stream, a);
@@ -240,8 +247,8 @@ hipError_t append_t(const AppendArgs& a0, hipStream_t stream) {
   AppendArgs a = a0;
   const int rows = (a.q != nullptr ? a.hq : 0) + 2 * a.hkv;
   a.run = head_run(a.n, rows, 64 / (D * (int)sizeof(T) / 32));
-  const dim3 grid((unsigned)((a.n + kRotThreads / 64 - 1) / (kRotThreads / 64)),
-                  (unsigned)((rows + a.run - 1) / a.run));
+  const dim3 grid = token_grid((a.n + kRotThreads / 64 - 1) / (kRotThreads / 64),
+                               (rows + a.run - 1) / a.run);
   hipLaunchKernelGGL((paged_append_kernel<T, D>), grid, dim3(kRotThreads), 0, stream, a);
   return hipGetLastError();
 }

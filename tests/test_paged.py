@@ -682,3 +682,35 @@ def test_no_tokens(cuda):
         P.pbb_paged_attention(desc, pos, table, q, *pages, torch.empty_like(q), q_start=start)
     for t, b in zip(pages, before):
         assert torch.equal(bits(t).cpu(), b)
+
+
+def test_more_threads_than_a_grid_row(cuda):
+    """Calls whose tokens need more threads than the first dimension of a grid holds (2^26 tokens, a
+    wave each): the last tokens' rows are those of a call of their own."""
+    n, last = 1 << 26, 5
+    d, heads = 128, 5
+    rope = P.make_rope(d, BASE)
+    positions = torch.arange(n + last, dtype=torch.int32, device=cuda)
+    x = torch.empty(n + last, heads, d, dtype=BF, device=cuda)        # 86 GB, turned in place
+    x[-last:] = torch.randn(last, heads, d, device=cuda).to(BF)
+    want = P.pbb_rotate(rope, positions[-last:], x[-last:].clone(), torch.empty_like(x[-last:]))
+    P.pbb_rotate(rope, positions, x, x)
+    assert torch.equal(bits(x[-last:]).cpu(), bits(want).cpu())
+    del x, positions
+    torch.cuda.empty_cache()
+
+    d, page = 64, 16
+    desc = P.make_paged_desc(2, 1, 1, d, page_size=page, n_pages=1, table_width=1)
+    kv = torch.empty(n + last, 1, d, dtype=BF, device=cuda)           # 8.6 GB
+    kv[-last:] = torch.randn(last, 1, d, device=cuda).to(BF)
+    kp, vp = P.alloc_pages(desc)
+    kp.zero_(), vp.zero_()
+    pos = torch.tensor([-1, 3], dtype=torch.int32, device=cuda)       # the first brings rows that no page takes
+    q_start = torch.tensor([0, n, n + last], dtype=torch.int32, device=cuda)
+    table = torch.zeros(2, 1, dtype=torch.int32, device=cuda)
+    P.pbb_paged_append(desc, pos, table, kv, kv, kp, vp, q_start=q_start)
+    for t in (kp, vp):
+        assert torch.equal(bits(t[0, 0, 3:3 + last]).cpu(), bits(kv[-last:, 0]).cpu())
+        assert not t[0, 0, :3].any() and not t[0, 0, 3 + last:].any()
+    del kv
+    torch.cuda.empty_cache()

@@ -100,7 +100,7 @@ def test_rotate_refusals():
         assert _rotate(**kw) == ALIGN, kw
 
 
-BAD_SHAPES = [dict(batch=0), dict(n_kv_heads=0), dict(n_q_heads=0), dict(n_q_heads=7), dict(n_q_heads=34),
+BAD_SHAPES = [dict(batch=0), dict(batch=(1 << 24) + 1), dict(n_kv_heads=0), dict(n_q_heads=0), dict(n_q_heads=7), dict(n_q_heads=34),
               dict(head_dim=96), dict(page_size=0), dict(page_size=8), dict(page_size=24),
               dict(page_size=(1 << 20) + 16),
               dict(n_pages=0), dict(table_width=0), dict(page_size=1 << 20, table_width=1 << 12),
@@ -275,3 +275,16 @@ def test_no_tokens():
     assert _append(n=0, k=0, v=0, rope=_rope(), pos=0, table=0) == 0
     assert _attend(n=0, q=0, out=0) == 0
     assert _rotate(n=0, x=0, out=0, heads=0) == SHAPE and _attend(_desc(batch=0), n=0) == SHAPE
+
+
+def test_attention_launch_limit():
+    """A launch has fewer than 2^32 threads: no more than 2^23 tiles in all KV heads."""
+    n = 1 << 23
+    assert _attend(_desc(batch=n), n=n) == SHAPE                              # 2 KV heads
+    assert _attend(_desc(batch=n // 2 + 1), n=n // 2 + 1, q=0) == SHAPE
+    assert _attend(_desc(batch=n // 2), n=n // 2, q=0) == NULL                # as many as there may be
+    assert _attend(_desc(batch=1), n=1 << 27, q=0) == NULL                    # 32 tokens a tile
+    assert _attend(_desc(batch=1), n=(1 << 27) + 1, q=0) == SHAPE
+    assert _attend(_desc(batch=1, dtype=B.DTYPE_F32), n=1 << 27) == SHAPE
+    assert _attend(_desc(batch=n), n=n // 2, q_start=A) == SHAPE
+    assert _append(_desc(batch=n), n=n, k=0) == NULL
