@@ -130,7 +130,8 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     uint32_t count = 0;
     round([&](int, const Chunk& c) {
       const int nt = p.tiles_of(c);
-      sum += (float)nt * (float)p.steps_of(a.shape, c);
+      // (contracted by hand: the merge launch works out the same pieces from the same sum)
+      sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, c), sum);
       count += (uint32_t)nt;
       return true;
     });
@@ -182,9 +183,9 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
 }
 
 // Merges the `ways` partial states of a tile ([COLS][D] outputs, then (reference, sum) per column,
-// `stride` floats apart) into rows of the output: store(column, channel, x, y, z, w) takes 4
-// channels of a column, lse(column, value) its log-partition in log2 units.  Every thread sums 4
-// channels of a column, eight states' loads in flight at a time.
+// `stride` floats apart) into rows of the output: store(column, channel, o, l) takes 4 channels of a
+// column, unnormalised, and its sum, lse(column, reference, l) the reference (log2 units) and the sum.
+// Every thread sums 4 channels of a column, eight states' loads in flight at a time.
 template <int D, int COLS, int THREADS, typename S, typename L>
 __device__ __forceinline__ void merge_states(const float* s0, size_t stride, int ways, int cols,
                                              int tid, S&& store, L&& lse) {
