@@ -542,7 +542,8 @@ def pbb_paged_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, q_s
                      rope_pos=None, q=None, q_out=None, stream=None):
     """Append the new tokens of every sequence to the cache (see ``include/pbb.h``): ``k``, ``v``
     [tokens][Hkv][d] packed by ``q_start`` (None: the same number for every sequence), ``rope``
-    applied to ``k`` and, into ``q_out``, to ``q`` [tokens][Hq][d]."""
+    applied to ``k`` and, into ``q_out``, to ``q`` [tokens][Hq][d], at ``rope_pos`` (int32
+    [axes][tokens], or [tokens] for one axis; None: the cache positions)."""
     dev = _device_for("k", k, "[tokens][Hkv][d]")
     n = k.shape[0]
     hq, hkv, d, dtype = _expect_paged(desc, pos, table, q_start, k_pages, v_pages, dev)
@@ -556,7 +557,8 @@ def pbb_paged_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, q_s
     if rope_pos is not None:
         if rope is None:
             raise ValueError("pbb_paged_append: rope_pos without rope")
-        _dense("rope_pos", rope_pos, (rope.n_axes, n), torch.int32, dev)
+        one = rope.n_axes == 1 and isinstance(rope_pos, torch.Tensor) and rope_pos.dim() == 1
+        _dense("rope_pos", rope_pos, (n,) if one else (rope.n_axes, n), torch.int32, dev)
     status = load_library().pbb_paged_append(
         desc, n, pos.data_ptr(), _ptr(q_start), table.data_ptr(), rope, _ptr(rope_pos), _ptr(q), qs,
         _ptr(q_out), k.data_ptr(), ks, v.data_ptr(), vs, k_pages.data_ptr(), v_pages.data_ptr(),

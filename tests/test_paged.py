@@ -670,7 +670,7 @@ def test_no_tokens(cuda):
     """A step that brings nothing."""
     desc = P.make_paged_desc(2, 4, 2, 64, page_size=16, n_pages=3, table_width=2)
     pages = P.alloc_pages(desc)
-    before = [bits(t).cpu() for t in pages]
+    before = [bits(t).copy() for t in pages]
     pos = torch.zeros(2, dtype=torch.int32, device=cuda)
     table = torch.zeros(2, 2, dtype=torch.int32, device=cuda)
     q_start = torch.zeros(3, dtype=torch.int32, device=cuda)
@@ -681,7 +681,7 @@ def test_no_tokens(cuda):
                            q_out=q)
         P.pbb_paged_attention(desc, pos, table, q, *pages, torch.empty_like(q), q_start=start)
     for t, b in zip(pages, before):
-        assert torch.equal(bits(t).cpu(), b)
+        assert (bits(t) == b).all()
 
 
 def test_more_threads_than_a_grid_row(cuda):
@@ -695,7 +695,7 @@ def test_more_threads_than_a_grid_row(cuda):
     x[-last:] = torch.randn(last, heads, d, device=cuda).to(BF)
     want = P.pbb_rotate(rope, positions[-last:], x[-last:].clone(), torch.empty_like(x[-last:]))
     P.pbb_rotate(rope, positions, x, x)
-    assert torch.equal(bits(x[-last:]).cpu(), bits(want).cpu())
+    assert (bits(x[-last:]) == bits(want)).all()
     del x, positions
     torch.cuda.empty_cache()
 
@@ -710,7 +710,25 @@ def test_more_threads_than_a_grid_row(cuda):
     table = torch.zeros(2, 1, dtype=torch.int32, device=cuda)
     P.pbb_paged_append(desc, pos, table, kv, kv, kp, vp, q_start=q_start)
     for t in (kp, vp):
-        assert torch.equal(bits(t[0, 0, 3:3 + last]).cpu(), bits(kv[-last:, 0]).cpu())
+        assert (bits(t[0, 0, 3:3 + last]) == bits(kv[-last:, 0])).all()
         assert not t[0, 0, :3].any() and not t[0, 0, 3 + last:].any()
     del kv
     torch.cuda.empty_cache()
+
+
+def test_append_positions_of_one_axis(cuda):
+    """[tokens] and [1][tokens] are the same positions; those of the cache are the ones left out."""
+    desc = P.make_paged_desc(1, 4, 2, 64, page_size=16, n_pages=2, table_width=2)
+    rope = P.make_rope(64, BASE)
+    pos = torch.tensor([7], dtype=torch.int32, device=cuda)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device=cuda)
+    kv = torch.randn(12, 2, 64, device=cuda).to(BF)
+    at = torch.arange(7, 19, dtype=torch.int32, device=cuda)
+    got = []
+    for rope_pos in (None, at, at[None]):
+        pages = [t.zero_() for t in P.alloc_pages(desc)]
+        P.pbb_paged_append(desc, pos, table, kv, kv, *pages, rope=rope, rope_pos=rope_pos)
+        got.append(torch.stack(pages).cpu())
+    assert got[0].any() and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    with pytest.raises(ValueError):
+        P.pbb_paged_append(desc, pos, table, kv, kv, *P.alloc_pages(desc), rope=rope, rope_pos=at[:-1])
