@@ -90,8 +90,9 @@ constexpr int kPagedMaxPieces = 2048;   // budget of a call's KV heads together,
 
 // Tile and cutting rules of a kind of kernel.  Where the even share of one round of the chip is short
 // (below many_least), C is that share, at least few_least: T / (round - tiles), so that tiles and pieces
-// together are no more than the round (half of the round, where the tiles alone are that many).  Else C = max(many_least, T / pieces): as many pieces as even out the end of the call, but
-// none so short that its first loads and its merge cost more than that gains.
+// together are no more than the round (half of the round, where the tiles alone are that many).  Else
+// C = max(many_least, T / pieces): as many pieces as even out the end of the call, but none so short
+// that its first loads and its merge cost more than that gains.
 struct PagedKind {
   int cols;     // query columns of a tile
   int step;     // keys per step, 16 or 32

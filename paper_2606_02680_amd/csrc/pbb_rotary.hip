@@ -94,9 +94,9 @@ __device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&
   hi = Piece<T>::put(oy);
 }
 
-// Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token has
-// fewer heads than a wave takes rows, a wave takes several tokens (2 heads, d 64, 16000 tokens with 12
-// query heads: 20.9 us for both calls with one token per wave, 15.9 with eight).
+// Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token
+// has fewer heads than a wave takes rows, a wave takes several tokens (2 heads, d 64, 16000 tokens with
+// 12 query heads: 20.9 us for both calls with one token per wave, 15.9 with eight).
 template <typename T, int D, bool NT>
 __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   constexpr int PC = D * (int)sizeof(T) / 32;   // pieces per half row
@@ -105,7 +105,8 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   const int lane = threadIdx.x & 63;
   const int row = lane / PC;
   const int sub = a.tokens_per_wave > 1 ? a.by_heads.div(row) : 0;   // token within the wave's
-  const int64_t tok = ((int64_t)token_group() * (kRotThreads / 64) + (threadIdx.x >> 6)) * a.tokens_per_wave + sub;
+  const int64_t wave = (int64_t)token_group() * (kRotThreads / 64) + (threadIdx.x >> 6);
+  const int64_t tok = wave * a.tokens_per_wave + sub;
   if (tok >= a.n || sub >= a.tokens_per_wave) return;
   const int pc = lane % PC;
   float cs[Piece<T>::N], sn[Piece<T>::N];
