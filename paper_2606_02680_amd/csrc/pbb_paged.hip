@@ -763,7 +763,82 @@ void paged_narrow_kernel(PagedArgs a) {
   narrow_walk<D, true>(a, it, g, smem);
 }
 
+// The summary of a call of many sequences (PlanWord), one workgroup: the steps and tiles of all of
+// them, which say how walks are cut, then the running sums over rounds of 64, a round to a wave.  Sums
+// stop at 2^30, above any item (see kMostItems).
+constexpr int kPlanWaves = 16;
+__global__ __launch_bounds__(kPlanWaves * 64) void paged_plan_kernel(PagedArgs a) {
+  constexpr int KINDS = 2 * kPlanRows;
+  __shared__ float sm_steps[kPlanWaves];
+  __shared__ uint32_t sm_tiles[kPlanWaves];
+  __shared__ uint32_t sm_round[2][kPlanWaves][KINDS];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const PagedPlan& p = a.plan;
+  float sum = 0.0f;
+  uint32_t count = 0;
+  for (int b = tid; b < a.batch; b += kPlanWaves * 64) {
+    const Chunk c = chunk_at(a, b);
+    const uint32_t nt = (uint32_t)p.tiles_of(c);
+    sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, c), sum);
+    count = count + nt < kMostItems ? count + nt : kMostItems;
+  }
+  const float steps_w = wave_scan(sum);
+  const uint32_t tiles_w = wave_scan(count);
+  if (lane == 63) {
+    sm_steps[wave] = steps_w;
+    sm_tiles[wave] = tiles_w < kMostItems ? tiles_w : kMostItems;
+  }
+  __syncthreads();
+  float steps = 0.0f;
+  uint32_t tiles = 0;
+  for (int w = 0; w < kPlanWaves; ++w) steps += sm_steps[w], tiles += sm_tiles[w];
+  const float per_share = per_share_of(p, steps, tiles);
+
+  const int rounds = paged_rounds(a.batch);
+  uint32_t before = 0;   // lane k < KINDS: the sum of row k / 2, kind k mod 2, of the rounds before r0
+  for (int r0 = 0, buf = 0; r0 < rounds; r0 += kPlanWaves, buf ^= 1) {
+    const int r = r0 + wave;
+    const Chunk c = r < rounds ? chunk_at(a, 64 * r + lane) : Chunk{0, 0, 0};
+#pragma unroll
+    for (int narrow = 0; narrow < 2; ++narrow) {
+      const Share s = share_of_chunk(a, c, narrow != 0, per_share);
+      const uint32_t items = wave_scan(s.items), cut = wave_scan(s.cut), slots = wave_scan(s.slots);
+      if (lane == 63) {
+        sm_round[buf][wave][2 * kRowItems + narrow] = items;
+        sm_round[buf][wave][2 * kRowCut + narrow] = cut;
+        sm_round[buf][wave][2 * kRowSlots + narrow] = slots;
+      }
+    }
+    __syncthreads();   // (the other buffer is written after every wave has passed the next one)
+    if (lane < KINDS) {
+      uint32_t upto = before;
+      for (int w = 0; w < kPlanWaves; ++w) {
+        const uint32_t own = sm_round[buf][w][lane];
+        const uint32_t end = upto + own < (1u << 30) ? upto + own : 1u << 30;
+        if (w == wave && r < rounds)
+          plan_row(a, lane >> 1, lane & 1)[r] = (lane >> 1) == kRowSlots ? upto : end;
+        upto = end;
+      }
+      before = upto;
+    }
+  }
+  // (uniform calls have one kind, counted under both: only the first is searched)
+  if (wave == 0) {
+    if (lane == 0) a.rounds[kPlanShare] = __float_as_uint(per_share);
+    if (lane == 2 * kRowItems) a.rounds[kPlanItems] = before;
+    if (lane == 2 * kRowSlots) a.rounds[kPlanSlots] = before;
+    if (lane == 2 * kRowCut) a.rounds[kPlanCut] = before;
+  }
+}
+
 }  // namespace
+
+hipError_t launch_paged_plan(const PagedArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanWaves * 64), 0, stream, a);
+  return hipGetLastError();
+}
 
 namespace {
 

@@ -93,7 +93,10 @@ size_t states_of(const pbb_paged_desc_t* d, const pbb::PagedPlan& p) {
 
 // What any call may need: calls of few columns per sequence are all planned alike, of the others one of
 // a single token needs most (which of them a call is, its q_start decides).
-size_t workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
+struct Workspace {   // counters, `states` bytes of partial states, the sequences' summary
+  size_t bytes, states;
+};
+Workspace workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
   const int group = d->n_q_heads / d->n_kv_heads;
   const bool f32 = d->dtype == PBB_DTYPE_F32;
   const size_t narrow = states_of(
@@ -102,8 +105,11 @@ size_t workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
   const size_t wide = states_of(
       d, pbb::PagedPlan::make(s, pbb::paged_kind(f32, false, d->head_dim), d->batch, d->n_kv_heads, group,
                               1, true));
-  const size_t bytes = narrow > wide ? narrow : wide;
-  return bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;
+  Workspace w;
+  w.states = narrow > wide ? narrow : wide;
+  const size_t bytes = w.states + (size_t)pbb::paged_rounds_bytes(d->batch);
+  w.bytes = bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;
+  return w;
 }
 
 }  // namespace
@@ -224,7 +230,7 @@ pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t* desc, int32_t n_t
   if (desc == nullptr || bytes == nullptr) return PBB_ERR_NULL;
   const pbb_status_t st = check_paged(desc, n_tokens);
   if (st != PBB_OK) return st;
-  *bytes = workspace_of(desc, shape_of(desc));
+  *bytes = workspace_of(desc, shape_of(desc)).bytes;
   return PBB_OK;
 }
 
@@ -247,14 +253,18 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   if (!aligned(pos, 4) || !aligned(q_start, 4) || !aligned(table, 4) || !aligned(q, 16) ||
       !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) || !aligned(lse, 4))
     return PBB_ERR_ALIGN;
-  const size_t need = workspace_of(desc, a.shape);
+  const Workspace ws = workspace_of(desc, a.shape);
+  const size_t need = ws.bytes;
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
   const size_t states = states_of(desc, a.plan);
-  if (states > 0 && states + pbb::kPagedCounterBytes > need) return PBB_ERR_WORKSPACE;  // (never)
+  if (states > ws.states) return PBB_ERR_WORKSPACE;  // (never)
   a.counters = need > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
   a.states = need > 0 ? reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) +
                                                  pbb::kPagedCounterBytes)
+                      : nullptr;
+  a.rounds = need > 0 ? reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) +
+                                                    pbb::kPagedCounterBytes + ws.states)
                       : nullptr;
   a.pos = pos;
   a.q_start = q_start;
@@ -274,8 +284,10 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
                                          : (float)(1.0 / std::sqrt((double)desc->head_dim));
   a.scale_log2 = (float)((double)scale * 1.4426950408889634);  // log2(e)
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const hipError_t e = desc->dtype == PBB_DTYPE_F32 ? pbb::launch_paged_f32(a, desc->head_dim, s)
-                                                    : pbb::launch_paged_bf16(a, desc->head_dim, s);
+  hipError_t e = a.plan.planned ? pbb::launch_paged_plan(a, s) : hipSuccess;
+  if (e == hipSuccess)
+    e = desc->dtype == PBB_DTYPE_F32 ? pbb::launch_paged_f32(a, desc->head_dim, s)
+                                     : pbb::launch_paged_bf16(a, desc->head_dim, s);
   return e == hipSuccess ? PBB_OK : PBB_ERR_LAUNCH;
 }
 

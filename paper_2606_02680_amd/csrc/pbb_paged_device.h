@@ -83,13 +83,76 @@ struct PagedItem {
   Chunk c;
 };
 
-// Item `item` of a KV head (false: there are not that many).  Every wave finds it by itself, 64
-// sequences at a time: their counts of pieces, and a sum over the lanes.  Items go sequence by
-// sequence, those of more than kPagedNarrowCols columns first, whose pieces take longest (128 single
-// tokens and chunks of 665 and 577: 249 us, 267 in the sequences' order, 303 with both kinds in turn,
-// eight items of each); of one sequence, piece by piece from the last tile (the longest walk) to the
-// first, so that workgroups running side by side read the same keys.  CUT: the items are the tiles
-// whose walks are cut (piece 0).
+// How many of the n entries of `ends`, which never fall, are at most x: every lane of the wave takes
+// part, 64 entries are compared at a time.  (Entries that do fall still give a number of 0 .. n.)
+template <typename T>
+__device__ __forceinline__ int count_upto(const T* ends, int n, T x, int lane) {
+  int lo = 0;
+  while (n > 64) {   // the answer lies in lo .. lo + n
+    const int stride = (n + 63) >> 6;
+    const int i = (lane + 1) * stride - 1;
+    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < n && ends[lo + i] <= x)) * stride;
+    lo += k < n ? k : n;
+    n = stride < n - k ? stride : n > k ? n - k : 0;
+  }
+  return lo + __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < n && ends[lo + lane] <= x));
+}
+
+// Words of a planned call's summary (PagedPlan::planned), written by a launch before the attention's:
+// 1 / C; the items, partial states and cut tiles of the sequences of more than kPagedNarrowCols columns
+// (all sequences where every one brings the same number of tokens); and per round of 64 sequences
+// the running sums of the two kinds of sequences: items and cut tiles at its end, states before it.
+enum PlanWord { kPlanShare, kPlanItems, kPlanSlots, kPlanCut, kPlanRounds = 8 };
+enum PlanRow { kRowItems, kRowCut, kRowSlots, kPlanRows };
+__device__ __forceinline__ uint32_t* plan_row(const PagedArgs& a, int row, int narrow) {
+  return a.rounds + kPlanRounds + (size_t)(2 * row + narrow) * (size_t)paged_rounds(a.batch);
+}
+
+__device__ __forceinline__ Chunk chunk_at(const PagedArgs& a, int b) {
+  if (b >= a.batch) return Chunk{0, 0, 0};
+  const bool ragged = a.plan.uniform < 0;
+  return chunk_of(b, a.plan.uniform, ragged ? a.q_start[b] : 0, ragged ? a.q_start[b + 1] : 0, a.pos[b],
+                  a.n);
+}
+
+// What a sequence's chunk counts for among those of its kind: items, cut tiles, partial states.
+// (q_start entries out of order can name any number of tiles: no count passes kMostItems, which is
+// more than any launch has, so that sums over a wave stay below 2^31.)
+constexpr uint32_t kMostItems = 1u << 24;
+struct Share {
+  int tiles, ways;
+  uint32_t items, cut, slots;
+};
+__device__ __forceinline__ Share share_of_chunk(const PagedArgs& a, const Chunk& c, bool narrow,
+                                                float per_share) {
+  const PagedPlan& p = a.plan;
+  const bool mine = p.uniform >= 0 || (c.count <= p.narrow_tokens) == narrow;
+  Share s;
+  s.tiles = mine ? p.tiles_of(c) : 0;
+  s.ways = p.pieces_of(p.steps_of(a.shape, c), per_share);
+  const uint32_t pieces = (uint32_t)s.tiles * (uint32_t)s.ways;
+  s.items = pieces < kMostItems ? pieces : kMostItems;
+  s.cut = s.ways > 1 ? (uint32_t)s.tiles : 0u;
+  s.slots = s.ways > 1 ? pieces : 0u;
+  return s;
+}
+
+// 1 / C of a call of these many steps and tiles.  (q_start entries out of order can name more tiles
+// than the launch has room for: no walk is cut then, so that no merge takes the state of a piece that does
+// not run.)
+__device__ __forceinline__ float per_share_of(const PagedPlan& p, float steps, uint32_t tiles) {
+  return p.pieces > 0 && tiles <= (uint32_t)p.tiles ? 1.0f / p.share_of(steps) : 0.0f;
+}
+
+// Item `item` of a KV head (false: there are not that many).  Items go sequence by sequence, those of
+// more than kPagedNarrowCols columns first, whose pieces take longest (128 single tokens and chunks of
+// 665 and 577: 249 us, 267 in the sequences' order, 303 with both kinds in turn, eight items of each);
+// of one sequence, piece by piece from the last tile (the longest walk) to the first, so that workgroups
+// running side by side read the same keys.  CUT: the items are the tiles whose walks are cut (piece 0).
+//
+// Every wave finds its item by itself: the counts of 64 sequences at a time, one to a lane, and sums
+// over the lanes.  Up to kPagedScan sequences it does so from the first on; above, a launch before this
+// one has summed up the rounds of 64 (PlanWord), and the wave searches those sums for its round.
 template <bool CUT>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane, PagedItem& it) {
   const PagedPlan& p = a.plan;
@@ -97,89 +160,78 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     const int tiles = p.tiles_of(Chunk{0, p.uniform, 0});
     it.b = tiles == 1 ? item : item / tiles;
     if (it.b >= a.batch) return false;
-    it.tile = tiles - 1 - (item - it.b * tiles);
-    it.piece = 0;
-    it.ways = 1;
-    it.slot = 0;
     it.c = chunk_of(it.b, p.uniform, 0, 0, scalar_word(a.pos, (size_t)it.b), a.n);
+    it.ways = 1;
+    it.piece = 0;
+    it.tile = tiles - 1 - (item - it.b * tiles);
+    it.slot = 0;   // (the last store here and below: else the compiler keeps fields in memory)
     return true;
   }
-  auto chunk = [&](int b) -> Chunk {
-    if (b >= a.batch) return Chunk{0, 0, 0};
-    const bool ragged = p.uniform < 0;
-    return chunk_of(b, p.uniform, ragged ? a.q_start[b] : 0, ragged ? a.q_start[b + 1] : 0, a.pos[b],
-                    a.n);
-  };
-  // the first 128 sequences' chunks, their loads in flight together
-  constexpr int KEPT = 2;
-  Chunk kept[KEPT];
-#pragma unroll
-  for (int r = 0; r < KEPT; ++r) kept[r] = chunk(64 * r + lane);
-  auto round = [&](auto&& visit) {   // visit(first sequence, this lane's chunk): false ends it
-#pragma unroll
-    for (int r = 0; r < KEPT; ++r) {
-      if (64 * r >= a.batch) return;
-      if (!visit(64 * r, kept[r])) return;
-    }
-    for (int b0 = 64 * KEPT; b0 < a.batch; b0 += 64)
-      if (!visit(b0, chunk(b0 + lane))) return;
-  };
   float per_share = 0.0f;
+  uint32_t base = 0, sbase = 0;
+  // looks for the item among the sequences b0 .. b0 + 63 (this lane's chunk c) of a kind
+  auto found = [&](int b0, const Chunk& c, bool narrow) -> bool {
+    const Share s = share_of_chunk(a, c, narrow, per_share);
+    const uint32_t count = CUT ? s.cut : s.items;
+    const uint32_t upto = wave_scan(count), supto = wave_scan(s.slots);
+    const uint32_t all = (uint32_t)lane_value((int)upto, 63);
+    if ((uint32_t)item >= base + all) {
+      base += all;
+      sbase += (uint32_t)lane_value((int)supto, 63);
+      return false;
+    }
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)item < base + upto));
+    it.b = b0 + l;
+    it.c.row0 = lane_value(c.row0, l);
+    it.c.count = lane_value(c.count, l);
+    it.c.pos = lane_value(c.pos, l);
+    it.ways = lane_value(s.ways, l);
+    const int tiles = lane_value(s.tiles, l);
+    const int r = item - (int)(base + (uint32_t)lane_value((int)(upto - count), l));
+    it.piece = r / tiles;
+    it.tile = tiles - 1 - (r - it.piece * tiles);
+    it.slot = (int)(sbase + (uint32_t)lane_value((int)(supto - s.slots), l)) + it.tile * it.ways;
+    return true;
+  };
+  if (p.planned) {
+    const int32_t* const words = (const int32_t*)a.rounds;
+    per_share = __uint_as_float((uint32_t)scalar_word(words, kPlanShare));
+    const uint32_t wide = (uint32_t)scalar_word(words, CUT ? kPlanCut : kPlanItems);
+    const bool narrow = (uint32_t)item >= wide;
+    if (narrow && p.uniform >= 0) return false;
+    if (narrow) base = wide, sbase = (uint32_t)scalar_word(words, kPlanSlots);
+    const uint32_t* const ends = plan_row(a, CUT ? kRowCut : kRowItems, narrow);
+    const int round = count_upto(ends, paged_rounds(a.batch), (uint32_t)item - base, lane);
+    if (round >= paged_rounds(a.batch)) return false;
+    if (round > 0) base += (uint32_t)scalar_word((const int32_t*)ends, (size_t)(round - 1));
+    sbase += (uint32_t)scalar_word((const int32_t*)plan_row(a, kRowSlots, narrow), (size_t)round);
+    return found(64 * round, chunk_at(a, 64 * round + lane), narrow);
+  }
+  // the sequences' chunks, their loads in flight together
+  constexpr int ROUNDS = kPagedScan / 64;
+  static_assert(ROUNDS == 2, "two chunks to a lane");
+  Chunk kept[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) kept[r] = chunk_at(a, 64 * r + lane);
   if (p.pieces > 0) {
     float sum = 0.0f;
     uint32_t count = 0;
-    round([&](int, const Chunk& c) {
-      const int nt = p.tiles_of(c);
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const uint32_t nt = (uint32_t)p.tiles_of(kept[r]);
       // (contracted by hand: the merge launch works out the same pieces from the same sum)
-      sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, c), sum);
-      count += (uint32_t)nt;
-      return true;
-    });
-    const float total =
+      sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, kept[r]), sum);
+      count += nt < kMostItems ? nt : kMostItems;
+    }
+    const float steps =
         __uint_as_float((uint32_t)lane_value((int)__float_as_uint(wave_scan(sum)), 63));
-    const uint32_t tiles = (uint32_t)lane_value((int)wave_scan(count), 63);
-    // (q_start entries out of order can name more tiles than the launch has room for: no walk is
-    // cut then, so that no merge waits for a piece that does not run)
-    if (tiles <= (uint32_t)p.tiles) per_share = 1.0f / p.share_of(total);
+    per_share = per_share_of(p, steps, (uint32_t)lane_value((int)wave_scan(count), 63));
   }
-  uint32_t base = 0, sbase = 0;
-  bool found = false;
-  auto search = [&](auto&& mine) {   // among the sequences that mine(tokens) takes
-    round([&](int b0, const Chunk& c) {
-      const int nt = mine(c.count) ? p.tiles_of(c) : 0;
-      const int ways = p.pieces_of(p.steps_of(a.shape, c), per_share);
-      const uint32_t pieces = (uint32_t)nt * (uint32_t)ways;
-      const uint32_t cut = ways > 1 ? pieces : 0u;
-      const uint32_t count = !CUT ? pieces : ways > 1 ? (uint32_t)nt : 0u;
-      const uint32_t upto = wave_scan(count), supto = wave_scan(cut);
-      const uint32_t all = (uint32_t)lane_value((int)upto, 63);
-      if ((uint32_t)item >= base + all) {
-        base += all;
-        sbase += (uint32_t)lane_value((int)supto, 63);
-        return true;
-      }
-      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64((uint32_t)item < base + upto));
-      it.b = b0 + l;
-      it.c.row0 = lane_value(c.row0, l);
-      it.c.count = lane_value(c.count, l);
-      it.c.pos = lane_value(c.pos, l);
-      it.ways = lane_value(ways, l);
-      const int tiles = lane_value(nt, l);
-      const int r = item - (int)(base + (uint32_t)lane_value((int)(upto - count), l));
-      it.piece = r / tiles;
-      it.tile = tiles - 1 - (r - it.piece * tiles);
-      it.slot = (int)(sbase + (uint32_t)lane_value((int)(supto - cut), l)) + it.tile * it.ways;
-      found = true;
-      return false;
-    });
+  auto search = [&](bool narrow) -> bool {
+    if (found(0, kept[0], narrow)) return true;
+    return a.batch > 64 && found(64, kept[1], narrow);
   };
-  if (p.uniform >= 0) {
-    search([](int) { return true; });
-  } else {
-    search([&](int count) { return count > p.narrow_tokens; });
-    if (!found) search([&](int count) { return count <= p.narrow_tokens; });
-  }
-  return found;
+  return search(false) || (p.uniform < 0 && search(true));
 }
 
 // Merges the `ways` partial states of a tile ([COLS][D] outputs, then (reference, sum) per column,

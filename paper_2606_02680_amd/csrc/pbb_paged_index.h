@@ -88,6 +88,15 @@ struct PagedShape {
 constexpr int kPagedNarrowCols = 16;
 constexpr int kPagedMaxPieces = 2048;   // budget of a call's KV heads together, at most
 
+// Sequences that every workgroup looks through by itself for its item; calls of more are summed up by a
+// launch of one workgroup before the attention's, since that search grows with the square of the batch.
+constexpr int kPagedScan = 128;
+// Rounds of 64 sequences, and the bytes of their summary.
+PBB_HD int paged_rounds(int batch) { return (batch + 63) >> 6; }
+inline uint64_t paged_rounds_bytes(int batch) {
+  return batch > kPagedScan ? (32 + 24 * (uint64_t)paged_rounds(batch) + 15) / 16 * 16 : 0;
+}
+
 // Tile and cutting rules of a kind of kernel.  Where the even share of one round of the chip is short
 // (below many_least), C is that share, at least few_least: T / (round - tiles), so that tiles and pieces
 // together are no more than the round (half of the round, where the tiles alone are that many).  Else
@@ -112,6 +121,7 @@ struct PagedPlan {
   int uniform;   // tokens of every sequence, -1: q_start says
   int narrow;    // 1: at most kPagedNarrowCols columns per sequence
   int narrow_tokens;   // tokens of that many columns
+  int planned;   // 1: a launch of its own sums up the sequences (more than kPagedScan, and searched)
   int tiles;     // tiles of a call, at most
   int slots;     // partial states per KV head, at most
   FastDiv by_hkv, by_tq, by_group;
@@ -149,6 +159,7 @@ struct PagedPlan {
     p.pieces = longest_walk(s, k, p.tq) > worth && 2 * hkv <= kPagedMaxPieces
                    ? (round > many ? round : many) : 0;
     p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
+    p.planned = batch > kPagedScan && (ragged || p.pieces > 0);
     return p;
   }
   static int64_t longest_walk(const PagedShape& s, const PagedKind& k, int tq) {

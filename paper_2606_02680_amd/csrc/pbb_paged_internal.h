@@ -69,6 +69,7 @@ struct PagedArgs {
   float* lse;                 // optional [hq][n]
   uint32_t* counters;         // per partial state of a head, zero between launches
   float* states;              // partial states of cut walks
+  uint32_t* rounds;           // the sequences' summary (plan.planned)
   int64_t q_stride;
   int32_t n;
   int32_t batch;
@@ -108,6 +109,7 @@ constexpr size_t paged_state_bytes(int cols, int head_dim) {
 // Rotary rows, paged append, attention over a paged cache; head_dim 64 or 128.
 hipError_t launch_rotate(const RotateArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
 hipError_t launch_paged_append(const AppendArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
+hipError_t launch_paged_plan(const PagedArgs& a, hipStream_t stream);   // (before either of these two)
 hipError_t launch_paged_bf16(const PagedArgs& a, int32_t head_dim, hipStream_t stream);
 hipError_t launch_paged_f32(const PagedArgs& a, int32_t head_dim, hipStream_t stream);
 

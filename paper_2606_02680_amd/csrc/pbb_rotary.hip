@@ -11,7 +11,7 @@
 // all rows of the token that it visits.
 
 #include "pbb_device.h"
-#include "pbb_paged_internal.h"
+#include "pbb_paged_device.h"
 
 namespace pbb {
 namespace {
@@ -132,16 +132,10 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
   }
 }
 
-// The chunk that packed row `tok` belongs to, or -1: the number of sequences whose rows end at or
-// before it, 64 at a time (every lane of the wave takes part; q_start is non-decreasing).
+// The sequence that packed row `tok` belongs to, or -1: the number of sequences whose rows end at or
+// before it (every lane of the wave takes part; q_start never falls).
 __device__ __forceinline__ int sequence_of(const int32_t* q_start, int batch, int tok, int lane) {
-  int b = 0;
-  for (int b0 = 0; b0 < batch; b0 += 64) {
-    const bool before = b0 + lane < batch && q_start[b0 + lane + 1] <= tok;
-    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
-    b += k;
-    if (k < 64) break;
-  }
+  const int b = count_upto(q_start + 1, batch, tok, lane);
   if (b >= batch) return -1;
   return __builtin_amdgcn_readfirstlane(q_start[b]) <= tok ? b : -1;
 }
