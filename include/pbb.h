@@ -369,7 +369,8 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t *desc, int32_t n_tokens, co
 
 /*
  * Workspace bytes pbb_paged_attention needs for calls of up to n_tokens tokens (0 where no walk can
- * be long enough to be spread over several workgroups).  The first PBB_PAGED_COUNTER_BYTES must be
+ * be long enough to be spread over several workgroups and the batch is at most 128: the sequences of
+ * larger ones are summed up in it).  The first PBB_PAGED_COUNTER_BYTES must be
  * zero before the first call and every call leaves them zero, so one allocation serves every later
  * call on one stream, for any descriptor it is large enough for; calls that may run concurrently
  * (captured graphs among them) need separate workspaces.
@@ -383,7 +384,7 @@ pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_t
  * (pbb_paged_append): out_t = softmax over s in A(t) of (q_t . k_s * scale) applied to v_s, t the
  * token's position, A(t) = {0 .. t}, or A_PBB(t) (Eq.(pbb), h = block / 2), or
  * {max(0, t - window + 1) .. t}, without positions that have no page.  Query head i reads KV head
- * floor(i / G).  Single tokens, chunks and a mixture of both in one launch.
+ * floor(i / G).  Single tokens, chunks and a mixture of both in one call.
  *   q, out   [n_tokens][n_q_heads][head_dim], tokens of q q_stride ELEMENTS apart
  *   lse      optional float32 [n_q_heads][n_tokens]: log sum_{s in A(t)} e^{z_s}, natural log
  * A token with an empty support (every page dropped) gets a zero output and lse -inf.  What cached
