@@ -37,9 +37,6 @@ static_assert(kPagedCols == 16 * kPagedGroups * kPagedWaves && kPagedStep == 32,
 // LDS stages and waves per SIMD that the registers are budgeted for (see the prefill).
 constexpr int kPagedStages128 = 3, kPagedOcc128 = 3;
 constexpr int kPagedStages64 = 4, kPagedOcc64 = 4;
-// Starting reference of the running maximum (log2 units): finite and below any score.
-constexpr float kNoScore = -3.0e38f;
-
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
@@ -81,8 +78,7 @@ __device__ __forceinline__ void narrow_walk(const PagedArgs& a, const PagedItem&
   constexpr int TILE = 16 * ROWB;       // 16 rows of K or V
   constexpr int OPS = TILE / 1024;      // DMA instructions of a tile
   constexpr int COLS = kPagedNarrowCols;
-  constexpr int MERGE = NW * COLS * (D + 2) * 4;
-  static_assert(MERGE + 16 <= narrow_lds<D>(), "the merge of the waves fits their tiles");
+  static_assert(NarrowOut<uint16_t, D, NW>::LDS <= narrow_lds<D>(), "the waves' states fit their tiles");
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -95,22 +91,9 @@ __device__ __forceinline__ void narrow_walk(const PagedArgs& a, const PagedItem&
   const int tokens = it.c.count;
   const int64_t row0 = it.c.row0;
   const int cols = tokens * G;
-  auto address = [&](int col) -> int64_t {   // output row of a column
-    const int cp = pl.by_group.div(col);
-    return (row0 + cp) * a.hq + (int64_t)(g * G + col - cp * G);
-  };
-  auto lse_at = [&](int col) -> int64_t {
-    const int cp = pl.by_group.div(col);
-    return (int64_t)(g * G + col - cp * G) * a.n + row0 + cp;
-  };
-  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
-    if (it.piece > 0) return;
-    for (int i = tid; i < cols * (ROWB / 16); i += NW * 64) {
-      const int col = i / (ROWB / 16);
-      *(u32x4*)((unsigned char*)a.out + address(col) * ROWB + (i - col * (ROWB / 16)) * 16) =
-          u32x4{0u, 0u, 0u, 0u};
-    }
-    if (a.lse != nullptr && tid < cols) a.lse[lse_at(tid)] = kNegInf;
+  const NarrowOut<uint16_t, D, NW> result{a, it, g, cols};
+  if (it.c.pos < 0) {
+    result.skip(tid);
     return;
   }
 
@@ -296,72 +279,16 @@ __device__ __forceinline__ void narrow_walk(const PagedArgs& a, const PagedItem&
     }
   }
 
-  // The waves' states through LDS (Eq.(lse)); each thread takes 4 channels of a column.
   lsum = sum_xor16_32(lsum);
   __syncthreads();   // every wave is done with its tiles
-  float* const sm_acc = (float*)smem;               // [NW][COLS][D]
-  float* const sm_m = sm_acc + NW * COLS * D;       // [NW][COLS]
-  float* const sm_l = sm_m + NW * COLS;
-  int* const last_one = (int*)(smem + MERGE);
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
-    *(f32x4*)(sm_acc + (wave * COLS + c16) * D + 16 * nb + 4 * j4) = acc[nb];
+    *(f32x4*)(result.outputs(smem) + (wave * COLS + c16) * D + 16 * nb + 4 * j4) = acc[nb];
   if (j4 == 0) {
-    sm_m[wave * COLS + c16] = m;
-    sm_l[wave * COLS + c16] = lsum;
+    result.references(smem)[wave * COLS + c16] = m;
+    result.sums(smem)[wave * COLS + c16] = lsum;
   }
-  __syncthreads();
-  constexpr int SCOLS = IN_PLACE ? COLS : kPagedCols;
-  constexpr size_t STATE = paged_state_bytes(SCOLS, D) / 4;
-  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
-  float* const part = a.states + (unit + it.piece) * STATE;
-  for (int i = tid; i < cols * (D / 4); i += NW * 64) {
-    const int col = i / (D / 4), q = i - col * (D / 4);
-    float M = kNoScore;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * COLS + col]);
-    float L = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {   // (a wave that saw nothing holds zeros)
-      const float wt = fast_exp2(sm_m[w * COLS + col] - M);
-      L += wt * sm_l[w * COLS + col];
-      o += wt * *(const f32x4*)(sm_acc + (w * COLS + col) * D + 4 * q);
-    }
-    if (it.ways == 1) {
-      store4((uint16_t*)a.out + address(col) * D + 4 * q, o, inverse_sum(L));
-      if (a.lse != nullptr && q == 0) a.lse[lse_at(col)] = log_partition(M, L);
-    } else if (IN_PLACE) {
-      coherent_store2(part + col * D + 4 * q, o[0], o[1]);
-      coherent_store2(part + col * D + 4 * q + 2, o[2], o[3]);
-      if (q == 0) coherent_store2(part + SCOLS * D + 2 * col, M, L);
-    } else {
-      *(f32x4*)(part + col * D + 4 * q) = o;
-      if (q == 0) *(float2*)(part + SCOLS * D + 2 * col) = make_float2(M, L);
-    }
-  }
-  if (!IN_PLACE || it.ways == 1) return;
-  // A cut walk: the count of its pieces; whoever completes it merges them (coherent_store2 says why
-  // this orders).
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
-  __syncthreads();
-  if (tid == 0) {
-    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-    *last_one = before == (unsigned)(it.ways - 1);
-    if (*last_one)
-      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!*last_one) return;
-  merge_states<D, SCOLS, NW * 64>(
-      a.states + unit * STATE, STATE, it.ways, cols, tid,
-      [&](int col, int c, f32x4 o, float l) {
-        store4((uint16_t*)a.out + address(col) * D + c, o, inverse_sum(l));
-      },
-      [&](int col, float mref, float l) {
-        if (a.lse != nullptr) a.lse[lse_at(col)] = log_partition(mref, l);
-      });
+  result.template finish<IN_PLACE, IN_PLACE ? COLS : kPagedCols>(tid, smem);
 }
 
 template <int D, int ST, int OCC>

@@ -71,6 +71,9 @@ __device__ __forceinline__ float wave_scan(float x) {
 }
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
+// Starting reference of a running maximum (log2 units): finite and below any score.
+constexpr float kNoScore = -3.0e38f;
+
 // A 32-bit word that the launch does not write, through the scalar cache.
 __device__ __forceinline__ int scalar_word(const int32_t* p, size_t i) {
   return ((const __attribute__((address_space(4))) int32_t*)(const void*)p)[i];
@@ -245,7 +248,7 @@ __device__ __forceinline__ void merge_states(const float* s0, size_t stride, int
   constexpr int U = 8;
   for (int i = tid; i < cols * Q; i += THREADS) {
     const int col = i / Q, q = i - col * Q;
-    float m = -3.0e38f, l = 0.0f;
+    float m = kNoScore, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int w0 = 0; w0 < ways; w0 += U) {
       float2 ml[U], x[U], y[U];
@@ -292,6 +295,109 @@ __device__ __forceinline__ void store4(uint16_t* p, f32x4 o, float scale) {
 }
 __device__ __forceinline__ void store4(float* p, f32x4 o, float scale) { *(f32x4*)p = o * scale; }
 
+// What a workgroup of a few-column walk (at most kPagedNarrowCols columns: all of a sequence's tokens
+// under a KV head, position-major, head-minor) does after its waves have walked, for both types.
+template <typename T, int D, int NW>
+struct NarrowOut {
+  static constexpr int COLS = kPagedNarrowCols;
+  static constexpr int LDS = NW * COLS * (D + 2) * 4 + 16;   // the waves' states, and a word
+  const PagedArgs& a;
+  const PagedItem& it;
+  int g;
+  int cols;
+
+  __device__ __forceinline__ int64_t address(int col) const {   // output row of a column
+    const int cp = a.plan.by_group.div(col);
+    return ((int64_t)it.c.row0 + cp) * a.hq + (int64_t)(g * a.group + col - cp * a.group);
+  }
+  __device__ __forceinline__ int64_t lse_at(int col) const {
+    const int cp = a.plan.by_group.div(col);
+    return (int64_t)(g * a.group + col - cp * a.group) * a.n + it.c.row0 + cp;
+  }
+
+  // A skipped sequence: zeros, no log-partition.
+  __device__ __forceinline__ void skip(int tid) const {
+    if (it.piece > 0) return;
+    constexpr int Q = D * (int)sizeof(T) / 16;
+    for (int i = tid; i < cols * Q; i += NW * 64) {
+      const int col = i / Q;
+      *(u32x4*)((unsigned char*)((T*)a.out + address(col) * D) + (i - col * Q) * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+    if (a.lse != nullptr && tid < cols) a.lse[lse_at(tid)] = kNegInf;
+  }
+
+  // The waves' states in LDS: unnormalised outputs [NW][COLS][D], references and sums [NW][COLS].
+  static __device__ __forceinline__ float* outputs(unsigned char* smem) { return (float*)smem; }
+  static __device__ __forceinline__ float* references(unsigned char* smem) {
+    return (float*)smem + NW * COLS * D;
+  }
+  static __device__ __forceinline__ float* sums(unsigned char* smem) {
+    return references(smem) + NW * COLS;
+  }
+
+  // Merges the waves' states (Eq.(lse)), each thread 4 channels of a column, once every wave has
+  // stored its own.  A cut walk leaves the result as the piece's state: IN_PLACE the last piece to end
+  // merges them, else a second launch does.
+  template <bool IN_PLACE, int SCOLS>
+  __device__ __forceinline__ void finish(int tid, unsigned char* smem) const {
+    const float* const sm_acc = outputs(smem);
+    const float* const sm_m = references(smem);
+    const float* const sm_l = sums(smem);
+    int* const last_one = (int*)(smem + LDS - 16);
+    __syncthreads();
+    constexpr size_t STATE = paged_state_bytes(SCOLS, D) / 4;
+    const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
+    float* const part = a.states + (unit + it.piece) * STATE;
+    for (int i = tid; i < cols * (D / 4); i += NW * 64) {
+      const int col = i / (D / 4), q = i - col * (D / 4);
+      float M = kNoScore;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * COLS + col]);
+      float L = 0.0f;
+      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {   // (a wave that saw nothing holds zeros)
+        const float wt = fast_exp2(sm_m[w * COLS + col] - M);
+        L += wt * sm_l[w * COLS + col];
+        o += wt * *(const f32x4*)(sm_acc + (w * COLS + col) * D + 4 * q);
+      }
+      if (it.ways == 1) {
+        store4((T*)a.out + address(col) * D + 4 * q, o, inverse_sum(L));
+        if (a.lse != nullptr && q == 0) a.lse[lse_at(col)] = log_partition(M, L);
+      } else if (IN_PLACE) {
+        coherent_store2(part + col * D + 4 * q, o[0], o[1]);
+        coherent_store2(part + col * D + 4 * q + 2, o[2], o[3]);
+        if (q == 0) coherent_store2(part + SCOLS * D + 2 * col, M, L);
+      } else {
+        *(f32x4*)(part + col * D + 4 * q) = o;
+        if (q == 0) *(float2*)(part + SCOLS * D + 2 * col) = make_float2(M, L);
+      }
+    }
+    if (!IN_PLACE || it.ways == 1) return;
+    // Whoever completes the count of the walk's pieces merges them (coherent_store2 says why this
+    // orders).
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
+    __syncthreads();
+    if (tid == 0) {
+      const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
+                                                     __HIP_MEMORY_SCOPE_AGENT);
+      *last_one = before == (unsigned)(it.ways - 1);
+      if (*last_one)
+        __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!*last_one) return;
+    merge_states<D, SCOLS, NW * 64>(
+        a.states + unit * STATE, STATE, it.ways, cols, tid,
+        [&](int col, int c, f32x4 o, float l) {
+          store4((T*)a.out + address(col) * D + c, o, inverse_sum(l));
+        },
+        [&](int col, float mref, float l) {
+          if (a.lse != nullptr) a.lse[lse_at(col)] = log_partition(mref, l);
+        });
+  }
+};
+
 // Merges the states of cut walks, a launch of its own after the pieces': x = (cut tile, KV head), y =
 // runs of 16 columns (in turn where the grid has fewer), four to a wave.  Lane l takes channels
 // 64 i + 4 (l mod 16) .. +3 of column l / 16.
@@ -312,7 +418,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   for (int col = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 4); col < cols; col += (int)gridDim.y * 16) {
     const float* so = s + col * D + 4 * (lane & 15);
     const float* sm = s + COLS * D + 2 * col;
-    float m = -3.0e38f, l = 0.0f;
+    float m = kNoScore, l = 0.0f;
     f32x4 o[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};

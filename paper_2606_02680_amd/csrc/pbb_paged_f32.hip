@@ -20,7 +20,6 @@ namespace {
 constexpr int kF32Waves = 4;
 static_assert(kPagedColsF32 == 16 * kF32Waves && kPagedStepF32 == 16, "tile");
 constexpr int kF32Stages = 3;
-constexpr float kNoScore = -3.0e38f;
 
 __device__ __forceinline__ bool is_special(float x) {
   return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
@@ -30,8 +29,6 @@ __device__ __forceinline__ bool is_special(float x) {
 // a wave reads its rows straight into registers as operands (as the fp32 decode does: 64 contiguous
 // bytes of each of 16 key rows, 256 of each of 4 value rows per 16-byte load), the next step's loads in
 // flight while it computes.  Bound: HBM, by the register loads that 8 waves per CU hold in flight.
-constexpr int kF32Merge128 = kF32Waves * kPagedNarrowCols * (128 + 2) * 4 + 16;
-
 template <int D, bool IN_PLACE>
 __device__ __forceinline__ void narrow_walk_f32(const PagedArgs& a, const PagedItem& it, int g,
                                                 unsigned char* smem) {
@@ -42,7 +39,6 @@ __device__ __forceinline__ void narrow_walk_f32(const PagedArgs& a, const PagedI
   constexpr int VQ = E / 4;     // and of each of its four value rows
   constexpr int ROWB = D * 4;
   constexpr int COLS = kPagedNarrowCols;
-  constexpr int MERGE = NW * COLS * (D + 2) * 4;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -55,22 +51,9 @@ __device__ __forceinline__ void narrow_walk_f32(const PagedArgs& a, const PagedI
   const int tokens = it.c.count;
   const int64_t row0 = it.c.row0;
   const int cols = tokens * G;
-  auto address = [&](int col) -> int64_t {   // output row of a column
-    const int cp = pl.by_group.div(col);
-    return (row0 + cp) * a.hq + (int64_t)(g * G + col - cp * G);
-  };
-  auto lse_at = [&](int col) -> int64_t {
-    const int cp = pl.by_group.div(col);
-    return (int64_t)(g * G + col - cp * G) * a.n + row0 + cp;
-  };
-  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
-    if (it.piece > 0) return;
-    for (int i = tid; i < cols * (D / 4); i += NW * 64) {
-      const int col = i / (D / 4);
-      *(f32x4*)((float*)a.out + address(col) * D + (i - col * (D / 4)) * 4) =
-          f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    if (a.lse != nullptr && tid < cols) a.lse[lse_at(tid)] = kNegInf;
+  const NarrowOut<float, D, NW> result{a, it, g, cols};
+  if (it.c.pos < 0) {
+    result.skip(tid);
     return;
   }
 
@@ -224,80 +207,24 @@ __device__ __forceinline__ void narrow_walk_f32(const PagedArgs& a, const PagedI
     }
   }
 
-  // The waves' states through LDS (Eq.(lse)).
   lsum = sum_xor16_32(lsum);
-  float* const sm_acc = (float*)smem;               // [NW][COLS][D]
-  float* const sm_m = sm_acc + NW * COLS * D;       // [NW][COLS]
-  float* const sm_l = sm_m + NW * COLS;
-  int* const last_one = (int*)(smem + MERGE);
 #pragma unroll
   for (int y = 0; y < E / 4; ++y)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *(f32x4*)(sm_acc + (wave * COLS + c16) * D + 64 * y + 16 * j4 + 4 * i) =
+      *(f32x4*)(result.outputs(smem) + (wave * COLS + c16) * D + 64 * y + 16 * j4 + 4 * i) =
           f32x4{acc[4 * y][i], acc[4 * y + 1][i], acc[4 * y + 2][i], acc[4 * y + 3][i]};
   if (j4 == 0) {
-    sm_m[wave * COLS + c16] = m;
-    sm_l[wave * COLS + c16] = lsum;
+    result.references(smem)[wave * COLS + c16] = m;
+    result.sums(smem)[wave * COLS + c16] = lsum;
   }
-  __syncthreads();
-  constexpr int SCOLS = IN_PLACE ? COLS : kPagedColsF32;
-  constexpr size_t STATE = paged_state_bytes(SCOLS, D) / 4;
-  const size_t unit = (size_t)it.slot * a.hkv + (size_t)g * it.ways;   // the tile's states lie together
-  float* const part = a.states + (unit + it.piece) * STATE;
-  for (int i = tid; i < cols * (D / 4); i += NW * 64) {
-    const int col = i / (D / 4), q = i - col * (D / 4);
-    float M = kNoScore;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w * COLS + col]);
-    float L = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {   // (a wave that saw nothing holds zeros)
-      const float wt = fast_exp2(sm_m[w * COLS + col] - M);
-      L += wt * sm_l[w * COLS + col];
-      o += wt * *(const f32x4*)(sm_acc + (w * COLS + col) * D + 4 * q);
-    }
-    if (it.ways == 1) {
-      store4((float*)a.out + address(col) * D + 4 * q, o, inverse_sum(L));
-      if (a.lse != nullptr && q == 0) a.lse[lse_at(col)] = log_partition(M, L);
-    } else if (IN_PLACE) {
-      coherent_store2(part + col * D + 4 * q, o[0], o[1]);
-      coherent_store2(part + col * D + 4 * q + 2, o[2], o[3]);
-      if (q == 0) coherent_store2(part + SCOLS * D + 2 * col, M, L);
-    } else {
-      *(f32x4*)(part + col * D + 4 * q) = o;
-      if (q == 0) *(float2*)(part + SCOLS * D + 2 * col) = make_float2(M, L);
-    }
-  }
-  if (!IN_PLACE || it.ways == 1) return;
-  // A cut walk: whoever completes the count of its pieces merges them (coherent_store2 says why this
-  // orders).
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's stores have completed
-  __syncthreads();
-  if (tid == 0) {
-    const unsigned before = __hip_atomic_fetch_add(&a.counters[unit], 1u, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-    *last_one = before == (unsigned)(it.ways - 1);
-    if (*last_one)
-      __hip_atomic_store(&a.counters[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!*last_one) return;
-  merge_states<D, SCOLS, NW * 64>(
-      a.states + unit * STATE, STATE, it.ways, cols, tid,
-      [&](int col, int c, f32x4 o, float l) {
-        store4((float*)a.out + address(col) * D + c, o, inverse_sum(l));
-      },
-      [&](int col, float mref, float l) {
-        if (a.lse != nullptr) a.lse[lse_at(col)] = log_partition(mref, l);
-      });
+  result.template finish<IN_PLACE, IN_PLACE ? COLS : kPagedColsF32>(tid, smem);
 }
 
 template <int D>
 __global__ __launch_bounds__(kF32Waves * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_narrow_f32_kernel(PagedArgs a) {
-  __shared__ __align__(1024) unsigned char smem[kF32Merge128];
+  __shared__ __align__(1024) unsigned char smem[NarrowOut<float, D, kF32Waves>::LDS];
   const int lane = threadIdx.x & 63;
   const int item = a.plan.by_hkv.div((int)blockIdx.x);
   const int g = (int)blockIdx.x - item * a.hkv;
@@ -335,7 +262,7 @@ void paged_f32_kernel(PagedArgs a) {
   PagedItem it;
   if (!find_item<false>(a, item, lane, it)) return;
   if (it.c.count <= pl.narrow_tokens) {
-    static_assert(sizeof(smem) >= kF32Waves * kPagedNarrowCols * (D + 2) * 4, "LDS");
+    static_assert(sizeof(smem) >= NarrowOut<float, D, NW>::LDS - 16, "LDS");   // (no word: not merged here)
     narrow_walk_f32<D, false>(a, it, g, smem);
     return;
   }
