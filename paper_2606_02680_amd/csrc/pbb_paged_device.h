@@ -132,7 +132,7 @@ __device__ __forceinline__ Share share_of_chunk(const PagedArgs& a, const Chunk&
   const bool mine = p.uniform >= 0 || (c.count <= p.narrow_tokens) == narrow;
   Share s;
   s.tiles = mine ? p.tiles_of(c) : 0;
-  s.ways = p.pieces_of(p.steps_of(a.shape, c), per_share);
+  s.ways = p.pieces > 0 ? p.pieces_of(p.steps_of(a.shape, c), per_share) : 1;
   const uint32_t pieces = (uint32_t)s.tiles * (uint32_t)s.ways;
   s.items = pieces < kMostItems ? pieces : kMostItems;
   s.cut = s.ways > 1 ? (uint32_t)s.tiles : 0u;
@@ -176,7 +176,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
   auto found = [&](int b0, const Chunk& c, bool narrow) -> bool {
     const Share s = share_of_chunk(a, c, narrow, per_share);
     const uint32_t count = CUT ? s.cut : s.items;
-    const uint32_t upto = wave_scan(count), supto = wave_scan(s.slots);
+    const uint32_t upto = wave_scan(count), supto = p.pieces > 0 ? wave_scan(s.slots) : 0u;
     const uint32_t all = (uint32_t)lane_value((int)upto, 63);
     if ((uint32_t)item >= base + all) {
       base += all;
@@ -221,6 +221,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     uint32_t count = 0;
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
+      if (64 * r >= a.batch) break;
       const uint32_t nt = (uint32_t)p.tiles_of(kept[r]);
       // (contracted by hand: the merge launch works out the same pieces from the same sum)
       sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, kept[r]), sum);
