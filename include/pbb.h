@@ -387,7 +387,8 @@ pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_t
  * floor(i / G).  Single tokens, chunks and a mixture of both in one call.
  *   q, out   [n_tokens][n_q_heads][head_dim], tokens of q q_stride ELEMENTS apart
  *   lse      optional float32 [n_q_heads][n_tokens]: log sum_{s in A(t)} e^{z_s}, natural log
- * A token with an empty support (every page dropped) gets a zero output and lse -inf.  What cached
+ * A token with an empty support (every page dropped) gets a zero output and lse -inf; one whose scores
+ * are all -inf NaN (0 / 0) and lse -inf.  What cached
  * rows outside a token's support hold (NaN and infinities included) does not reach its output.
  * float32: fp32 arithmetic throughout; bfloat16: fp32 accumulation, weights rounded to bf16 for the
  * value products, output RNE.  workspace: pbb_paged_workspace_bytes bytes, 16-byte aligned (NULL if

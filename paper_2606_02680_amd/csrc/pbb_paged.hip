@@ -288,7 +288,7 @@ __device__ __forceinline__ void narrow_walk(const PagedArgs& a, const PagedItem&
     result.references(smem)[wave * COLS + c16] = m;
     result.sums(smem)[wave * COLS + c16] = lsum;
   }
-  result.template finish<IN_PLACE, IN_PLACE ? COLS : kPagedCols>(tid, smem);
+  result.template finish<IN_PLACE, IN_PLACE ? COLS : kPagedCols>(tid, smem, 16 * h0, 16 * h1 - 1);
 }
 
 template <int D, int ST, int OCC>
@@ -636,13 +636,19 @@ void paged_bf16_kernel(PagedArgs a) {
     }
   }
 
-  // Output of a column: o = acc / l (bf16 RNE), lse = (m + log2 l) * ln 2; an empty support has l 0
-  // and gets zeros and -inf.
+  // Output of a column: o = acc / l (bf16 RNE), lse = (m + log2 l) * ln 2.
+#pragma unroll
+  for (int qc = 0; qc < QC; ++qc) {
+    lsum[qc] = sum_xor16_32(lsum[qc]);
+    if (__builtin_expect(lsum[qc] == 0.0f, 0) && any_page(sh, table, max(lo_c[qc], s_first * 32),
+                                     min(tcol[qc], (s_first + nsteps) * 32 - 1)))
+      m[qc] = kNoWeight;
+  }
   if (it.ways == 1) {
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
-      const float l = sum_xor16_32(lsum[qc]);
-      const float inv = inverse_sum(l);
+      const float l = lsum[qc];
+      const float inv = inverse_sum(m[qc], l);
       u32x4 w[NB / 2];
 #pragma unroll
       for (int q = 0; q < NB / 2; ++q) w[q] = pair_blocks(acc[qc][2 * q], acc[qc][2 * q + 1], inv);
@@ -666,7 +672,7 @@ void paged_bf16_kernel(PagedArgs a) {
       a.states + ((size_t)it.slot * a.hkv + (size_t)g * it.ways + it.piece) * STATE;
 #pragma unroll
   for (int qc = 0; qc < QC; ++qc) {
-    const float l = sum_xor16_32(lsum[qc]);
+    const float l = lsum[qc];
     const int col = (wave * QC + qc) * 16 + c16;
     if (col < cols) {
 #pragma unroll

@@ -71,8 +71,9 @@ __device__ __forceinline__ float wave_scan(float x) {
 }
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// Starting reference of a running maximum (log2 units): finite and below any score.
-constexpr float kNoScore = -3.0e38f;
+// Starting reference of a running maximum (log2 units): finite and below any score; and that of a
+// column which has seen keys, but only with scores of -inf: its sum is 0 like that of one without keys.
+constexpr float kNoScore = -3.0e38f, kNoWeight = -2.9e38f;
 
 // A 32-bit word that the launch does not write, through the scalar cache.
 __device__ __forceinline__ int scalar_word(const int32_t* p, size_t i) {
@@ -238,9 +239,23 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
   return search(false) || (p.uniform < 0 && search(true));
 }
 
+// Whether one of the positions first .. last has a page: what a column whose sum is 0 asks about its keys.
+__device__ __forceinline__ bool any_page(const PagedShape& sh, const int32_t* table, int first, int last) {
+  last = min(last, sh.capacity - 1);
+  if (last < first) return false;
+  const int end = sh.by_page.div(last);
+  for (int i = sh.by_page.div(first); i <= end; i += 8) {
+    bool any = false;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) any |= sh.is_page(table[min(i + u, end)]);
+    if (any) return true;
+  }
+  return false;
+}
+
 // Merges the `ways` partial states of a tile ([COLS][D] outputs, then (reference, sum) per column,
-// `stride` floats apart) into rows of the output: store(column, channel, o, l) takes 4 channels of a
-// column, unnormalised, and its sum, lse(column, reference, l) the reference (log2 units) and the sum.
+// `stride` floats apart) into rows of the output: store(column, channel, o, reference, l) takes 4 channels
+// of a column, unnormalised, its reference (log2 units) and its sum, lse(column, reference, l) these two.
 // Every thread sums 4 channels of a column, eight states' loads in flight at a time.
 template <int D, int COLS, int THREADS, typename S, typename L>
 __device__ __forceinline__ void merge_states(const float* s0, size_t stride, int ways, int cols,
@@ -279,14 +294,16 @@ __device__ __forceinline__ void merge_states(const float* s0, size_t stride, int
         }
       }
     }
-    store(col, 4 * q, o, l);
+    store(col, 4 * q, o, m, l);
     if (q == 0) lse(col, m, l);
   }
 }
 
-// 1 / l and the natural-log partition of a column with reference m and sum l; an empty support has
-// l 0 and gets zeros and -inf.
-__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+// 1 / l and the natural-log partition of a column with reference m and sum l.  An empty support has l 0
+// and gets zeros and -inf; one whose scores are all -inf (kNoWeight) NaN, 0 / 0, and -inf.
+__device__ __forceinline__ float inverse_sum(float m, float l) {
+  return l != 0.0f ? 1.0f / l : m > kNoScore ? __builtin_nanf("") : 0.0f;
+}
 __device__ __forceinline__ float log_partition(float m, float l) {
   return l == 0.0f ? kNegInf : (m + __builtin_log2f(l)) * 0.69314718055994531f;
 }
@@ -337,10 +354,10 @@ struct NarrowOut {
   }
 
   // Merges the waves' states (Eq.(lse)), each thread 4 channels of a column, once every wave has
-  // stored its own.  A cut walk leaves the result as the piece's state: IN_PLACE the last piece to end
+  // stored its own (positions first .. last).  A cut walk leaves the result as the piece's state: IN_PLACE the last piece to end
   // merges them, else a second launch does.
   template <bool IN_PLACE, int SCOLS>
-  __device__ __forceinline__ void finish(int tid, unsigned char* smem) const {
+  __device__ __forceinline__ void finish(int tid, unsigned char* smem, int first, int last) const {
     const float* const sm_acc = outputs(smem);
     const float* const sm_m = references(smem);
     const float* const sm_l = sums(smem);
@@ -362,8 +379,14 @@ struct NarrowOut {
         L += wt * sm_l[w * COLS + col];
         o += wt * *(const f32x4*)(sm_acc + (w * COLS + col) * D + 4 * q);
       }
+      if (__builtin_expect(L == 0.0f, 0)) {
+        const int t = it.c.pos + a.plan.by_group.div(col);
+        if (any_page(a.shape, a.table + (size_t)it.b * a.shape.width, max(first, a.shape.support_lo(t)),
+                     min(last, t)))
+          M = kNoWeight;
+      }
       if (it.ways == 1) {
-        store4((T*)a.out + address(col) * D + 4 * q, o, inverse_sum(L));
+        store4((T*)a.out + address(col) * D + 4 * q, o, inverse_sum(M, L));
         if (a.lse != nullptr && q == 0) a.lse[lse_at(col)] = log_partition(M, L);
       } else if (IN_PLACE) {
         coherent_store2(part + col * D + 4 * q, o[0], o[1]);
@@ -390,8 +413,8 @@ struct NarrowOut {
     if (!*last_one) return;
     merge_states<D, SCOLS, NW * 64>(
         a.states + unit * STATE, STATE, it.ways, cols, tid,
-        [&](int col, int c, f32x4 o, float l) {
-          store4((T*)a.out + address(col) * D + c, o, inverse_sum(l));
+        [&](int col, int c, f32x4 o, float mref, float l) {
+          store4((T*)a.out + address(col) * D + c, o, inverse_sum(mref, l));
         },
         [&](int col, float mref, float l) {
           if (a.lse != nullptr) a.lse[lse_at(col)] = log_partition(mref, l);
@@ -457,7 +480,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     const int cp = pl.by_group.div(col);
     const int64_t row = (int64_t)it.c.row0 + p0 + cp;
     const int head = g * a.group + col - cp * a.group;
-    const float inv = inverse_sum(l);
+    const float inv = inverse_sum(m, l);
     T* out = (T*)a.out + (row * a.hq + head) * D + 4 * (lane & 15);
 #pragma unroll
     for (int i = 0; i < NB; ++i) store4(out + 64 * i, o[i], inv);

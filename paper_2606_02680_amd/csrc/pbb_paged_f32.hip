@@ -218,7 +218,7 @@ __device__ __forceinline__ void narrow_walk_f32(const PagedArgs& a, const PagedI
     result.references(smem)[wave * COLS + c16] = m;
     result.sums(smem)[wave * COLS + c16] = lsum;
   }
-  result.template finish<IN_PLACE, IN_PLACE ? COLS : kPagedColsF32>(tid, smem);
+  result.template finish<IN_PLACE, IN_PLACE ? COLS : kPagedColsF32>(tid, smem, 16 * s0, 16 * s1 - 1);
 }
 
 template <int D>
@@ -482,9 +482,11 @@ void paged_f32_kernel(PagedArgs a) {
 
   // Lane (c16, j4) holds channels 64 y + 16 j4 + 4 i + x in acc[4 y + x][i].
   const float l = sum_xor16_32(lsum);
+  if (__builtin_expect(l == 0.0f, 0) && any_page(sh, table, max(lo_c, s_first * 16), min(tcol, (s_first + nsteps) * 16 - 1)))
+    m = kNoWeight;
   if (it.ways == 1) {
     if (valid) {
-      const float inv = inverse_sum(l);
+      const float inv = inverse_sum(m, l);
       float* o = (float*)a.out + address(col) * D + 16 * j4;
 #pragma unroll
       for (int y = 0; y < E / 4; ++y)
