@@ -368,12 +368,12 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t *desc, int32_t n_tokens, co
                               void *stream);
 
 /*
- * Workspace bytes pbb_paged_attention needs for calls of up to n_tokens tokens (0 where no walk can
- * be long enough to be spread over several workgroups and the batch is at most 128: the sequences of
- * larger ones are summed up in it).  The first PBB_PAGED_COUNTER_BYTES must be
- * zero before the first call and every call leaves them zero, so one allocation serves every later
- * call on one stream, for any descriptor it is large enough for; calls that may run concurrently
- * (captured graphs among them) need separate workspaces.
+ * Workspace bytes pbb_paged_attention needs for calls with this descriptor, whatever they bring: n_tokens
+ * is checked as such a call's, and the size is the same for all (0 where no walk can be long enough to be
+ * spread over several workgroups and the batch is at most 128: the sequences of larger ones are summed
+ * up in it).  The first PBB_PAGED_COUNTER_BYTES must be zero before the first call and every call leaves
+ * them zero, so one allocation serves every later call on one stream, for any descriptor it is large
+ * enough for; calls that may run concurrently (captured graphs among them) need separate workspaces.
  */
 #define PBB_PAGED_COUNTER_BYTES 65536u
 pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_tokens,

@@ -330,8 +330,7 @@ void paged_bf16_kernel(PagedArgs a) {
   const int64_t row0 = (int64_t)it.c.row0 + p0;                 // packed row of the first one
   const int cols = tokens * G;
 
-  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
-    if (it.piece > 0) return;
+  if (it.c.pos < 0) {   // a skipped sequence, never cut: zeros, no log-partition
     for (int i = tid; i < cols * (ROWB / 16); i += NW * 64) {
       const int col = i / (ROWB / 16), pc = i - col * (ROWB / 16);
       const int cp = pl.by_group.div(col);

@@ -92,7 +92,8 @@ size_t states_of(const pbb_paged_desc_t* d, const pbb::PagedPlan& p) {
 }
 
 // What any call may need: calls of few columns per sequence are all planned alike, of the others one of
-// a single token needs most (which of them a call is, its q_start decides).
+// a single token needs most (which of them a call is, its q_start decides).  So the size depends on the
+// descriptor alone.
 struct Workspace {   // counters, `states` bytes of partial states, the sequences' summary
   size_t bytes, states;
 };
@@ -257,8 +258,6 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   const size_t need = ws.bytes;
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
-  const size_t states = states_of(desc, a.plan);
-  if (states > ws.states) return PBB_ERR_WORKSPACE;  // (never)
   a.counters = need > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
   a.states = need > 0 ? reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) +
                                                  pbb::kPagedCounterBytes)

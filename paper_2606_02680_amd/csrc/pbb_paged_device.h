@@ -333,9 +333,8 @@ struct NarrowOut {
     return (int64_t)(g * a.group + col - cp * a.group) * a.n + it.c.row0 + cp;
   }
 
-  // A skipped sequence: zeros, no log-partition.
+  // A skipped sequence (one step by PagedPlan::steps_of, so never cut): zeros, no log-partition.
   __device__ __forceinline__ void skip(int tid) const {
-    if (it.piece > 0) return;
     constexpr int Q = D * (int)sizeof(T) / 16;
     for (int i = tid; i < cols * Q; i += NW * 64) {
       const int col = i / Q;

@@ -279,8 +279,7 @@ void paged_f32_kernel(PagedArgs a) {
     return (int64_t)(g * G + col - cp * G) * a.n + row0 + cp;
   };
 
-  if (it.c.pos < 0) {   // a skipped sequence: zeros, no log-partition
-    if (it.piece > 0) return;
+  if (it.c.pos < 0) {   // a skipped sequence, never cut: zeros, no log-partition
     for (int i = tid; i < cols * PPR; i += NW * 64) {
       const int col = i / PPR;
       *(f32x4*)((unsigned char*)a.out + address(col) * ROWB + (i - col * PPR) * 16) =

@@ -514,9 +514,9 @@ PAGED_COUNTER_BYTES = 65536
 
 
 def alloc_paged_workspace(desc: PbbPagedDesc, n_tokens: int, device="cuda"):
-    """Workspace for :func:`pbb_paged_attention` calls of up to ``n_tokens`` tokens, its counters
-    zero, or None when they need none.  Calls leave the counters zero, so one allocation serves every
-    later call on one stream (calls that may overlap need their own)."""
+    """Workspace for :func:`pbb_paged_attention` calls with ``desc``, its counters zero, or None when they
+    need none; the same for every ``n_tokens``.  Calls leave the counters zero, so one allocation
+    serves every later call on one stream (calls that may overlap need their own)."""
     n = paged_workspace_bytes(desc, n_tokens)
     if n == 0:
         return None
