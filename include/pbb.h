@@ -390,8 +390,9 @@ pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_t
  * A token with an empty support (every page dropped) gets a zero output and lse -inf; one whose scores
  * are all -inf NaN (0 / 0) and lse -inf.  What cached
  * rows outside a token's support hold (NaN and infinities included) does not reach its output.
- * float32: fp32 arithmetic throughout; bfloat16: fp32 accumulation, weights rounded to bf16 for the
- * value products, output RNE.  workspace: pbb_paged_workspace_bytes bytes, 16-byte aligned (NULL if
+ * float32: fp32 arithmetic throughout; bfloat16: fp32 accumulation, output RNE, and for the value
+ * products weights rounded to bf16 (sequences of at most 16 / G tokens, G = n_q_heads / n_kv_heads, in
+ * a call: to 15 bits or more).  workspace: pbb_paged_workspace_bytes bytes, 16-byte aligned (NULL if
  * 0; PBB_ERR_WORKSPACE if NULL or smaller otherwise).  out must not overlap an input.
  */
 pbb_status_t pbb_paged_attention(const pbb_paged_desc_t *desc, int32_t n_tokens,
