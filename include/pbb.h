@@ -273,7 +273,8 @@ pbb_status_t swa_backward(const pbb_desc_t *desc, int32_t n, const void *q, cons
  * decode steps) turns by turns[c] * p whole turns, p the position of the token on axis axis[c]:
  * text has one axis, images and video have time, height and width.  pbb_rope_init fills the
  * struct for rates base^(-2c / head_dim) / (2 pi); a caller may change turns[] afterwards (scaled
- * contexts: any finite rates) and axis[].  The struct is plain data, read on the host at each call.
+ * contexts: any rates below 2^992 in size, PBB_ERR_SHAPE otherwise) and axis[].  The struct is plain
+ * data, read on the host at each call.
  */
 #define PBB_MAX_AXES 4
 typedef struct {

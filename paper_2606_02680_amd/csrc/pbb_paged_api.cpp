@@ -35,8 +35,8 @@ bool known_dtype(int32_t dtype) { return dtype == PBB_DTYPE_F32 || dtype == PBB_
 pbb_status_t check_rope(const pbb_rope_t* r, int32_t head_dim) {
   if (r->head_dim != head_dim) return PBB_ERR_SHAPE;
   if (r->n_axes < 1 || r->n_axes > PBB_MAX_AXES) return PBB_ERR_SHAPE;
-  for (int c = 0; c < head_dim / 2; ++c)
-    if (r->axis[c] >= r->n_axes || !std::isfinite(r->turns[c])) return PBB_ERR_SHAPE;
+  for (int c = 0; c < head_dim / 2; ++c)   // (below 2^992 no position's turns pass the largest double)
+    if (r->axis[c] >= r->n_axes || !(std::fabs(r->turns[c]) < 0x1p992)) return PBB_ERR_SHAPE;
   return PBB_OK;
 }
 
