@@ -571,7 +571,7 @@ def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out
                         lse=None, workspace=None, stream=None):
     """Attention of the new tokens over the cache that holds them (see ``include/pbb.h``): ``q``,
     ``out`` [tokens][Hq][d] packed by ``q_start``; optional ``lse`` [Hq][tokens] (float32).
-    Allocates the workspace when none is given."""
+    ``workspace``: of :func:`alloc_paged_workspace`, contiguous; allocated when none is given."""
     dev = _device_for("q", q, "[tokens][Hq][d]")
     n = q.shape[0]
     hq, _, d, dtype = _expect_paged(desc, pos, table, q_start, k_pages, v_pages, dev)
@@ -582,6 +582,8 @@ def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out
     ws_bytes = 0
     if workspace is not None:
         _expect_on("workspace", workspace, dev)
+        if not workspace.is_contiguous():   # (its bytes would not be numel of them, one after another)
+            raise ValueError("workspace: must be contiguous")
         ws_bytes = workspace.numel() * workspace.element_size()
     elif n > 0 and paged_workspace_bytes(desc, n) > 0:
         workspace = _scratch_on(stream, lambda: alloc_paged_workspace(desc, n, q.device))
