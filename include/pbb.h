@@ -318,7 +318,8 @@ pbb_status_t pbb_rotate(const pbb_rope_t *rope, int32_t n_tokens, int32_t n_head
  * memory.  An entry outside [0, n_pages) is no page: positions it would hold are not stored by an
  * append and lie outside every support (pages may be dropped, also from the middle of a sequence);
  * so are positions from table_width * page_size on.  Sequences may share pages that no call of
- * pbb_paged_append writes at the same time.
+ * pbb_paged_append writes at the same time; of two tokens of a call that share a row (a table that names
+ * a page twice) either, or a mixture, is stored.
  *
  * Tokens of a call are packed: sequence b brings rows q_start[b] .. q_start[b+1] - 1 of the packed
  * tensors, token i of them at position pos[b] + i.  q_start: int32 [batch + 1], device memory,
@@ -370,11 +371,12 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t *desc, int32_t n_tokens, co
 
 /*
  * Workspace bytes pbb_paged_attention needs for calls with this descriptor, whatever they bring: n_tokens
- * is checked as such a call's, and the size is the same for all (0 where no walk can be long enough to be
- * spread over several workgroups and the batch is at most 128: the sequences of larger ones are summed
- * up in it).  The first PBB_PAGED_COUNTER_BYTES must be zero before the first call and every call leaves
- * them zero, so one allocation serves every later call on one stream, for any descriptor it is large
- * enough for; calls that may run concurrently (captured graphs among them) need separate workspaces.
+ * is checked as such a call's, and the size is the same for all.  0 where no walk can be long enough to
+ * be spread over several workgroups and the batch is at most 128; the sequences of a larger batch are
+ * summed up in it, which calls without q_start do without (and take NULL) where walks are that short.
+ * The first PBB_PAGED_COUNTER_BYTES must be zero before the first call and every call leaves them zero, so
+ * one allocation serves every later call on one stream, for any descriptor it is large enough for; calls
+ * that may run concurrently (captured graphs among them) need separate workspaces.
  */
 #define PBB_PAGED_COUNTER_BYTES 65536u
 pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_tokens,

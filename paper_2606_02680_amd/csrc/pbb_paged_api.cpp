@@ -255,7 +255,8 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
       !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) || !aligned(lse, 4))
     return PBB_ERR_ALIGN;
   const Workspace ws = workspace_of(desc, a.shape);
-  const size_t need = ws.bytes;
+  const size_t own = ws.states + (a.plan.planned ? (size_t)pbb::paged_rounds_bytes(desc->batch) : 0);
+  const size_t need = own > 0 ? pbb::kPagedCounterBytes + own : 0;
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
   a.counters = need > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
