@@ -14,9 +14,9 @@
 // through narrow_walk, in the same launch.
 //
 // Bound: with many columns the matrix and vector work of a step at the clock that the card's power
-// allows (16384 tokens, 32/8 heads, d 128: 1872 to 1965 us over the boxes measured, 1120 to 1175
-// TFLOP/s, matrix cores 0.52 busy at 1.97 GHz); with few columns HBM (192 single tokens at up to 32768:
-// 1865 us, 6.7 TB/s).
+// allows (16384 tokens, 32/8 heads, d 128: 1872 to 2240 us over the boxes measured, 980 to 1175
+// TFLOP/s, matrix cores 0.51 busy at 1.9 GHz); with few columns HBM (192 single tokens at up to 32768:
+// 1876 us, 6.7 TB/s).
 //
 // Masks.  Steps with a key outside some column's support set its scores to -inf.  What such keys hold
 // is unknown (rows never written, dropped pages), and 0 * inf or 0 * NaN would reach the products, so

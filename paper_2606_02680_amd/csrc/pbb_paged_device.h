@@ -353,8 +353,8 @@ struct NarrowOut {
   }
 
   // Merges the waves' states (Eq.(lse)), each thread 4 channels of a column, once every wave has
-  // stored its own (positions first .. last).  A cut walk leaves the result as the piece's state: IN_PLACE the last piece to end
-  // merges them, else a second launch does.
+  // stored its own; they have walked positions first .. last.  A cut walk leaves the result as the
+  // piece's state: IN_PLACE the last piece to end merges them, else a second launch does.
   template <bool IN_PLACE, int SCOLS>
   __device__ __forceinline__ void finish(int tid, unsigned char* smem, int first, int last) const {
     const float* const sm_acc = outputs(smem);

@@ -481,7 +481,8 @@ void paged_f32_kernel(PagedArgs a) {
 
   // Lane (c16, j4) holds channels 64 y + 16 j4 + 4 i + x in acc[4 y + x][i].
   const float l = sum_xor16_32(lsum);
-  if (__builtin_expect(l == 0.0f, 0) && any_page(sh, table, max(lo_c, s_first * 16), min(tcol, (s_first + nsteps) * 16 - 1)))
+  if (__builtin_expect(l == 0.0f, 0) &&
+      any_page(sh, table, max(lo_c, s_first * 16), min(tcol, (s_first + nsteps) * 16 - 1)))
     m = kNoWeight;
   if (it.ways == 1) {
     if (valid) {

@@ -26,7 +26,7 @@ dim3 token_grid(int64_t groups, int runs) {
 }
 // Rows of more bytes than the last-level cache (256 MB) are read and written with the non-temporal
 // hint: what is written first is gone before anything reads it (4 x 16384 tokens of 32 heads, d 128:
-// 537 MB, 259 us with the 8 key heads' call, 235 with the hint, 5.7 TB/s; 16000 tokens, 131 MB: the
+// 537 MB, 259 us with the 8 key heads' call, 239 to 241 with the hint, 5.6 TB/s; 16000 tokens, 131 MB: the
 // next kernel finds them in the cache).
 constexpr int64_t kStreamBytes = 256ll << 20;
 
@@ -175,7 +175,9 @@ __global__ __launch_bounds__(kRotThreads) void paged_append_kernel(AppendArgs a)
   const int hq = a.q != nullptr ? a.hq : 0;
   const int rows = hq + 2 * a.hkv;
   const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
-  constexpr int AU = 2;   // rows of a lane in flight (one: 49.5 us at 37 sequences' 9000 tokens, two 47)
+  // rows of a lane in flight (one: 49.5 us at 37 sequences' 9000 tokens, two 47, both with the inputs in the
+  // last-level cache; 55 from memory)
+  constexpr int AU = 2;
   const int64_t page_row = page < 0 ? 0 : (int64_t)page * a.hkv * a.shape.page_size + slot;
   for (int r0 = blockIdx.y * a.run + lane / PC; r0 < r1; r0 += AU * ROWS) {
     u32x4 lo[AU], hi[AU];
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(kRotThreads) void paged_append_kernel(AppendArgs a)
 
 // Heads per workgroup row of the grid: all of a token's, unless the tokens alone leave the chip
 // short of waves; then as few as a wave takes at once, and no more than 65535 runs (2000 tokens of 48
-// rows: 11.5 us, 13.5 with a run per 8 rows; 256 tokens: 5.0 us so).
+// rows: 11.5 us, 13.5 with a run per 8 rows; 256 tokens: 5.0 us so; inputs in the last-level cache).
 int head_run(int tokens, int heads, int rows) {
   if (tokens >= 1024) return heads;
   const int least = (heads + 65534) / 65535;
