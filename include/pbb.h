@@ -372,7 +372,7 @@ pbb_status_t pbb_paged_append(const pbb_paged_desc_t *desc, int32_t n_tokens, co
 /*
  * Workspace bytes pbb_paged_attention needs for calls with this descriptor, whatever they bring: n_tokens
  * is checked as such a call's, and the size is the same for all.  0 where no walk can be long enough to
- * be spread over several workgroups and the batch is at most 128; the sequences of a larger batch are
+ * be spread over several workgroups and the batch is at most 384; the sequences of a larger batch are
  * summed up in it, which calls without q_start do without (and take NULL) where walks are that short.
  * The first PBB_PAGED_COUNTER_BYTES must be zero before the first call and every call leaves them zero, so
  * one allocation serves every later call on one stream, for any descriptor it is large enough for; calls

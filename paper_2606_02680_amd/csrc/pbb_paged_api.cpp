@@ -108,7 +108,8 @@ Workspace workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
                               1, true));
   Workspace w;
   w.states = narrow > wide ? narrow : wide;
-  const size_t bytes = w.states + (size_t)pbb::paged_rounds_bytes(d->batch);
+  const int scanned = w.states > 0 ? pbb::kPagedScan : pbb::kPagedScanUncut;   // (PagedPlan::planned)
+  const size_t bytes = w.states + (d->batch > scanned ? (size_t)pbb::paged_rounds_bytes(d->batch) : 0);
   w.bytes = bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;
   return w;
 }

@@ -155,8 +155,8 @@ __device__ __forceinline__ float per_share_of(const PagedPlan& p, float steps, u
 // running side by side read the same keys.  CUT: the items are the tiles whose walks are cut (piece 0).
 //
 // Every wave finds its item by itself: the counts of 64 sequences at a time, one to a lane, and sums
-// over the lanes.  Up to kPagedScan sequences it does so from the first on; above, a launch before this
-// one has summed up the rounds of 64 (PlanWord), and the wave searches those sums for its round.
+// over the lanes.  In small batches it does so from the first on; in others (PagedPlan::planned) a launch
+// before this one has summed up the rounds of 64 (PlanWord), and the wave searches those for its round.
 template <bool CUT>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane, PagedItem& it) {
   const PagedPlan& p = a.plan;
@@ -211,30 +211,36 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int item, int lane
     sbase += (uint32_t)scalar_word((const int32_t*)plan_row(a, kRowSlots, narrow), (size_t)round);
     return found(64 * round, chunk_at(a, 64 * round + lane), narrow);
   }
-  // the sequences' chunks, their loads in flight together
-  constexpr int ROUNDS = kPagedScan / 64;
-  static_assert(ROUNDS == 2, "two chunks to a lane");
+  // the first 128 sequences' chunks, their loads in flight together
+  constexpr int ROUNDS = 2;
   Chunk kept[ROUNDS];
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) kept[r] = chunk_at(a, 64 * r + lane);
   if (p.pieces > 0) {
     float sum = 0.0f;
     uint32_t count = 0;
+    auto add = [&](const Chunk& c) {
+      const uint32_t nt = (uint32_t)p.tiles_of(c);
+      // (contracted by hand: the merge launch works out the same pieces from the same sum)
+      sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, c), sum);
+      count = count + nt < kMostItems ? count + nt : kMostItems;
+    };
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
       if (64 * r >= a.batch) break;
-      const uint32_t nt = (uint32_t)p.tiles_of(kept[r]);
-      // (contracted by hand: the merge launch works out the same pieces from the same sum)
-      sum = __builtin_fmaf((float)nt, (float)p.steps_of(a.shape, kept[r]), sum);
-      count += nt < kMostItems ? nt : kMostItems;
+      add(kept[r]);
     }
+    for (int b0 = 64 * ROUNDS; b0 < a.batch; b0 += 64) add(chunk_at(a, b0 + lane));
     const float steps =
         __uint_as_float((uint32_t)lane_value((int)__float_as_uint(wave_scan(sum)), 63));
     per_share = per_share_of(p, steps, (uint32_t)lane_value((int)wave_scan(count), 63));
   }
   auto search = [&](bool narrow) -> bool {
     if (found(0, kept[0], narrow)) return true;
-    return a.batch > 64 && found(64, kept[1], narrow);
+    if (a.batch > 64 && found(64, kept[1], narrow)) return true;
+    for (int b0 = 64 * ROUNDS; b0 < a.batch; b0 += 64)
+      if (found(b0, chunk_at(a, b0 + lane), narrow)) return true;
+    return false;
   };
   return search(false) || (p.uniform < 0 && search(true));
 }

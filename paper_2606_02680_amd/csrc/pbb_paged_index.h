@@ -90,13 +90,15 @@ constexpr int kPagedMaxPieces = 2048;   // budget of a call's KV heads together,
 
 // Sequences that every workgroup looks through by itself for its item; calls of more are summed up by a
 // launch of one workgroup before the attention's, since that search grows with the square of the batch
-// (single tokens named by q_start, 16/2 heads, d 128, 100 cached each: 256 of them 22.6 us, 33.3 with
-// every workgroup looking through all; 1024 41 / 120; 16384 434 / 10870; 128 21.7 without the launch).
-constexpr int kPagedScan = 128;
+// (single tokens named by q_start, 16/2 heads, d 128, 100 cached each, walks that may be cut: 132 of them
+// 22.2 us, 27.2 with every workgroup looking through all; 1024 41 / 120; 16384 434 / 10870).  Where every
+// sequence brings the same number the search is one pass shorter (192 19.6 / 19.2, 224 19.7 / 21.7), and
+// where no walk can be cut one more (256 21.8 / 19.6, 320 23.0 / 21.9, 512 26.2 / 30.9).
+constexpr int kPagedScan = 128, kPagedScanEqual = 192, kPagedScanUncut = 384;
 // Rounds of 64 sequences, and the bytes of their summary.
 PBB_HD int paged_rounds(int batch) { return (batch + 63) >> 6; }
 inline uint64_t paged_rounds_bytes(int batch) {
-  return batch > kPagedScan ? (32 + 24 * (uint64_t)paged_rounds(batch) + 15) / 16 * 16 : 0;
+  return (32 + 24 * (uint64_t)paged_rounds(batch) + 15) / 16 * 16;
 }
 
 // Tile and cutting rules of a kind of kernel.  Where the even share of one round of the chip is short
@@ -123,7 +125,7 @@ struct PagedPlan {
   int uniform;   // tokens of every sequence, -1: q_start says
   int narrow;    // 1: at most kPagedNarrowCols columns per sequence
   int narrow_tokens;   // tokens of that many columns
-  int planned;   // 1: a launch of its own sums up the sequences (more than kPagedScan, and searched)
+  int planned;   // 1: a launch of its own sums up the sequences
   int tiles;     // tiles of a call, at most
   int slots;     // partial states per KV head, at most
   FastDiv by_hkv, by_tq, by_group;
@@ -161,7 +163,8 @@ struct PagedPlan {
     p.pieces = longest_walk(s, k, p.tq) > worth && 2 * hkv <= kPagedMaxPieces
                    ? (round > many ? round : many) : 0;
     p.slots = p.pieces > 0 ? 2 * p.pieces + p.pieces / 8 + 2 : 0;
-    p.planned = batch > kPagedScan && (ragged || p.pieces > 0);
+    p.planned = p.pieces > 0 ? batch > (ragged ? kPagedScan : kPagedScanEqual)
+                             : ragged && batch > kPagedScanUncut;
     return p;
   }
   static int64_t longest_walk(const PagedShape& s, const PagedKind& k, int tq) {

@@ -39,12 +39,14 @@ int main() {
     const float total = (float)pick(1, 1 << 30);
     if (p.steps_of(s, skipped) != 1 || p.pieces_of(1, 1.0f / p.share_of(total)) != 1)
       return std::printf("skipped %d\n", i), 1;
-    if (p.planned && batch <= kPagedScan) return std::printf("planned %d\n", i), 1;
-    if (!p.planned && batch > kPagedScan && (ragged || p.pieces > 0)) return std::printf("search %d\n", i), 1;
+    // a summary only where the workspace has room for one; no search of the first kind in a large batch
+    if (p.planned && batch <= (most.slots > 0 ? kPagedScan : kPagedScanUncut))
+      return std::printf("planned %d\n", i), 1;
+    if (!p.planned && batch > kPagedScanUncut && (ragged || p.pieces > 0)) return std::printf("search %d\n", i), 1;
   }
   for (int batch : {1, 128, 129, 192, 193, 1 << 24}) {
     const uint64_t bytes = paged_rounds_bytes(batch), rounds = (uint64_t)paged_rounds(batch);
-    if (batch <= kPagedScan ? bytes != 0 : bytes < 4 * (8 + 6 * rounds) || bytes % 16 != 0)
+    if (bytes < 4 * (8 + 6 * rounds) || bytes % 16 != 0)
       return std::printf("rounds %d\n", batch), 1;
   }
   return 0;

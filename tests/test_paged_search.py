@@ -1,6 +1,6 @@
 """How the workgroups of a paged call find their work, on the GPU: batches of more sequences than a
-workgroup looks through by itself (a launch of its own sums them up), against the float64 reference; and
-that the search costs calls of many sequences next to nothing."""
+workgroup looks through by itself (a launch before it sums them up) and of fewer, against the float64
+reference; and that the search costs calls of many sequences next to nothing."""
 from __future__ import annotations
 
 import math
@@ -138,3 +138,21 @@ def test_cost_of_many_sequences(cuda):
     plain, ragged = _time(lambda: append(None, *pages[0])), _time(lambda: append(start, *pages[1]))
     print(f"[search] append {plain * 1e3:.0f} us, {ragged * 1e3:.0f} with q_start", flush=True)
     assert all(torch.equal(a, b) for a, b in zip(*pages)) and ragged < 4 * plain
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [64, 65, 200, 384, 385, 1025])
+def test_ragged_uncut(cuda, dtype, n):
+    """A table too short for walks to be cut: looked through up to 384 sequences, summed up above."""
+    lens = [(-1 if i % 50 == 7 else (i * 13) % 20, (1, 1, 0, 3, 40)[i % 5]) for i in range(n)]
+    c = Cache(lens, 4, 2, 64, 16, dtype, seed=n, before=1, behind=2, fill=math.nan)
+    assert (P.paged_workspace_bytes(c.desc(), c.n) > 0) == (n > 384)
+    _check(c, cuda)
+
+
+@pytest.mark.parametrize("n,new", [(140, 1), (192, 1), (193, 1), (140, 20)])
+def test_uniform_small(cuda, n, new):
+    """The same number of tokens each, walks that may be cut, looked through up to 192 sequences."""
+    lens = [((i * 7) % 30, new) for i in range(n)]
+    lens[n - 1], lens[130], lens[5] = (1500, new), (700, new), (-1, new)
+    _check(Cache(lens, 4, 1, 64, 16, BF, seed=n + new, uniform=True, fill=math.nan), cuda)

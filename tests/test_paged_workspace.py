@@ -28,10 +28,10 @@ def test_workspace_views(cuda):
     assert torch.equal(call(whole[:n]), call(None))
 
 
-@pytest.mark.parametrize("batch", [128, 300])
+@pytest.mark.parametrize("batch", [384, 500])
 def test_calls_without_a_workspace(cuda, batch):
     """Where no walk is long enough to be cut, calls of the same number of tokens per sequence take none, whatever
-    the batch; q_start needs one for more than 128 sequences."""
+    the batch; q_start needs one for more than 384 sequences."""
     c = Cache([(i % 40, 1) for i in range(batch)], 4, 2, 64, 16, BF, seed=batch, uniform=True)
     x, desc = c.on(cuda), c.desc()
     out = torch.full_like(x["q"], 9.0)
@@ -46,5 +46,5 @@ def test_calls_without_a_workspace(cuda, batch):
     want = P.pbb_paged_attention(desc, x["pos"], x["table"], x["q"], x["k_pages"], x["v_pages"],
                                  torch.empty_like(out), q_start=start)
     assert torch.equal(out, want)
-    assert call(start.data_ptr()) == (0 if batch == 128 else 5)
+    assert call(start.data_ptr()) == (0 if batch == 384 else 5)
     torch.cuda.synchronize()
