@@ -538,8 +538,8 @@ void paged_bf16_kernel(PagedArgs a) {
     // maxima (the accumulators rescaled, the weights taken again) only in a step where the
     // eight weights of some lane and column sum above 2^8 or to infinity.
     // The weights enter the products rounded to bf16, the sum in 32 bits: products of what the rounding
-    // leaves would be a third more matrix work and 10 more spilled registers (chunks 4.5 ms instead of
-    // 2.65, a 16384-token prompt 2.94 instead of 1.89; error against fp64 1.66e-3 instead of 2.34e-3).
+    // leaves would be half as much matrix work again and 10 more spilled registers (chunks 4.5 ms instead
+    // of 2.65, a 16384-token prompt 2.94 instead of 1.89; error against fp64 1.66e-3 instead of 2.34e-3).
     bf16x8 pB[QC];
     float ps[QC];
     auto weights = [&]() {
@@ -655,8 +655,8 @@ void paged_bf16_kernel(PagedArgs a) {
 #pragma unroll
   for (int qc = 0; qc < QC; ++qc) {
     lsum[qc] = sum_xor16_32(lsum[qc]);
-    if (__builtin_expect(lsum[qc] == 0.0f, 0) && any_page(sh, table, max(lo_c[qc], s_first * 32),
-                                     min(tcol[qc], (s_first + nsteps) * 32 - 1)))
+    if (__builtin_expect(lsum[qc] == 0.0f, 0) &&
+        any_page(sh, table, max(lo_c[qc], s_first * 32), min(tcol[qc], (s_first + nsteps) * 32 - 1)))
       m[qc] = kNoWeight;
   }
   if (it.ways == 1) {
