@@ -14,7 +14,7 @@
 // through narrow_walk, in the same launch.
 //
 // Bound: with many columns the matrix and vector work of a step at the clock that the card's power
-// allows (16384 tokens, 32/8 heads, d 128: 1872 to 2240 us over the boxes measured, 980 to 1175
+// allows (16384 tokens, 32/8 heads, d 128: 1872 to 2240 us over the cards measured, 980 to 1175
 // TFLOP/s, matrix cores 0.51 busy at 1.9 GHz); with few columns HBM (192 single tokens at up to 32768:
 // 1876 us, 6.7 TB/s).
 //
