@@ -248,7 +248,7 @@ def prepare(case, seed):
                                       n_pages=s["k_pages"].shape[0], table_width=s["table"].shape[1],
                                       block=c["block"], window=c["window"])
     if c["kind"] == "attend":
-        s["workspace"] = P.alloc_paged8_workspace(s["desc"], s["q"].shape[0], DEV)
+        s["workspace"] = P.alloc_coded_workspace(s["desc"], s["q"].shape[0], DEV)
     return s
 
 
@@ -291,26 +291,26 @@ def _own_grad(c, s):
 def _own_append(c, s):
     import paper_2606_02680_amd as P
     q, k, v = _parts(c, s["qkv"])
-    P.pbb_paged8_append(s["desc"], s["pos"], s["table"], k, v, s["k_pages"], s["v_pages"],
-                        s["k_scales"], s["v_scales"], q_start=s["q_start"], rope=s["rope"],
-                        rope_pos=s["rope_pos"], q=q, q_out=s["q_out"], q_weight=s["q_weight"],
-                        k_weight=s["k_weight"], eps=EPS)
+    P.pbb_coded_append(s["desc"], s["pos"], s["table"], k, v, s["k_pages"], s["v_pages"],
+                       s["k_scales"], s["v_scales"], q_start=s["q_start"], rope=s["rope"],
+                       rope_pos=s["rope_pos"], q=q, q_out=s["q_out"], q_weight=s["q_weight"],
+                       k_weight=s["k_weight"], eps=EPS)
     _own_read(c, s)
     return {"q_out": s["q_out"], "k": s["k"], "v": s["v"]}
 
 
 def _own_read(c, s):
     import paper_2606_02680_amd as P
-    P.pbb_paged8_read(s["desc"], s["pos"], s["table"], s["k_pages"], s["v_pages"], s["k_scales"],
-                      s["v_scales"], s["k"], s["v"], q_start=s["q_start"])
+    P.pbb_coded_read(s["desc"], s["pos"], s["table"], s["k_pages"], s["v_pages"], s["k_scales"],
+                     s["v_scales"], s["k"], s["v"], q_start=s["q_start"])
     return {"k": s["k"], "v": s["v"]}
 
 
 def _own_attend(c, s):
     import paper_2606_02680_amd as P
-    P.pbb_paged8_attention(s["desc"], s["pos"], s["table"], s["q"], s["k_pages"], s["v_pages"],
-                           s["k_scales"], s["v_scales"], s["out"], q_start=s["q_start"],
-                           lse=s["lse"], workspace=s["workspace"])
+    P.pbb_coded_attention(s["desc"], s["pos"], s["table"], s["q"], s["k_pages"], s["v_pages"],
+                          s["k_scales"], s["v_scales"], s["out"], q_start=s["q_start"],
+                          lse=s["lse"], workspace=s["workspace"])
     return {"out": s["out"], "lse": s["lse"]}
 
 
