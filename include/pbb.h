@@ -404,6 +404,115 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t *desc, int32_t n_tokens,
                                  const void *v_pages, void *out, float *lse, void *workspace,
                                  size_t workspace_bytes, void *stream);
 
+/*
+ * Norms of queries and keys for each head, with the rotation in the same pass: models that divide every
+ * query and key row by its root mean square before they turn it.
+ *   y = R(p) (x r w),  r = 1 / sqrt(mean_c x_c^2 + eps),  R(p) the rotation of pbb_rotate
+ * in fp32 (a row's squares are summed in fp32: magnitudes up to about 1e18), rounded once.  eps > 0 and
+ * finite (PBB_ERR_SHAPE otherwise).  q_weight, k_weight: [head_dim] of the rows' type, device memory, 16-byte
+ * aligned, NULL for ones.  The struct is plain data, read on the host at each call.
+ */
+typedef struct {
+  float eps;
+  const void *q_weight;
+  const void *k_weight;
+} pbb_norm_t;
+
+/*
+ * Norm and rotation of the query and the key rows of every token, one launch: what pbb_prefill,
+ * pbb_backward, their sliding-window counterparts and pbb_paged_append (without rope) expect of q and k.
+ *   q, q_out   [n_tokens][n_q_heads][head_dim], k, k_out [n_tokens][n_kv_heads][head_dim], tokens
+ *              *_stride ELEMENTS apart (as x_stride of pbb_rotate)
+ *   rope       NULL: no rotation (positions is ignored); positions: int32 [n_axes][n_tokens], any value
+ * n_kv_heads may be 0: then there are no keys, and k and k_out are ignored.  An output may be its input
+ * (with the same stride); other overlaps are undefined.  Both types.  Limits, sizes of nothing and
+ * alignment as pbb_rotate; head_dim 64 or 128.
+ */
+pbb_status_t pbb_norm_rotate(const pbb_norm_t *norm, const pbb_rope_t *rope, int32_t head_dim,
+                             int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                             const int32_t *positions, const void *q, int64_t q_stride, void *q_out,
+                             int64_t q_out_stride, const void *k, int64_t k_stride, void *k_out,
+                             int64_t k_out_stride, int32_t dtype, void *stream);
+
+/*
+ * Gradients of pbb_norm_rotate for upstream gradients q_grad and k_grad of its outputs, which its inputs q
+ * and k say all about (nothing is kept from the forward pass).  With g = R^T y_grad, a = g w, s = mean(a x) r:
+ *   dx = r (a - x r s),  dw = sum over tokens and heads of g x r
+ *   q_grad, dq, k_grad, dk   rows as q and k, with strides of their own; dq may be q_grad or q, dk k_grad
+ *              or k (same stride)
+ *   dq_weight, dk_weight     optional float32 [head_dim], 4-byte aligned, overwritten (zeros for
+ *              n_tokens == 0)
+ * Deterministic.  workspace: pbb_norm_workspace_bytes bytes, 16-byte aligned, contents irrelevant; needed
+ * with a weight's gradient only (PBB_ERR_WORKSPACE if NULL or smaller).  The size depends on the arguments
+ * of its query alone and is at most 4104 * head_dim.
+ */
+pbb_status_t pbb_norm_workspace_bytes(int32_t head_dim, int32_t n_tokens, int32_t n_q_heads,
+                                      int32_t n_kv_heads, int32_t dtype, size_t *bytes);
+
+pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t *norm, const pbb_rope_t *rope, int32_t head_dim,
+                                      int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                                      const int32_t *positions, const void *q, int64_t q_stride,
+                                      const void *q_grad, int64_t q_grad_stride, void *dq,
+                                      int64_t dq_stride, const void *k, int64_t k_stride,
+                                      const void *k_grad, int64_t k_grad_stride, void *dk,
+                                      int64_t dk_stride, float *dq_weight, float *dk_weight,
+                                      int32_t dtype, void *workspace, size_t workspace_bytes,
+                                      void *stream);
+
+/*
+ * 8-bit paged cache: the paged cache above with half the bytes.
+ *
+ * k_pages, v_pages [n_pages][n_kv_heads][page_size][head_dim] hold e4m3 codes (one byte: sign, 4 bits of
+ * exponent, bias 7, 3 of significand; no infinities, NaN is 0x7F and 0xFF), k_scales, v_scales
+ * [n_pages][n_kv_heads][page_size] a byte b per row: a value is its code times 2^(b - 127), which is exact in
+ * bfloat16.  Tables, packed tokens, pos, q_start, skipped sequences and limits are those of the paged cache;
+ * the descriptor's dtype, that of q, k, v and out, is PBB_DTYPE_BF16 (PBB_ERR_DTYPE otherwise).  All
+ * tensors 16-byte aligned, int32 arrays 4.
+ *
+ * What an append stores of a row: the least power 2^e, -100 <= e <= 119, under which the row's largest finite
+ * magnitude is at most 448 (the largest code), and the codes of the quotients, nearest, ties to even, finite
+ * ones cut to 448 (rows above 2^119 * 448) -- so each value to half a step, 2^-4 of itself, or 2^-10 of 2^e
+ * where that is more.  Infinities and NaN are stored as NaN.  Other writers may use any byte from 1 to 254.
+ *
+ * pbb_coded_append: arguments as pbb_paged_append; norm (optional) divides and weights keys and queries
+ * as pbb_norm_rotate does, before rope turns them, all in fp32 and rounded once: to codes (keys), to
+ * bfloat16 (q_out).  Values are quantised as they come.
+ */
+pbb_status_t pbb_coded_append(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
+                               const int32_t *q_start, const int32_t *table, const pbb_norm_t *norm,
+                               const pbb_rope_t *rope, const int32_t *rope_pos, const void *q,
+                               int64_t q_stride, void *q_out, const void *k, int64_t k_stride,
+                               const void *v, int64_t v_stride, void *k_pages, void *v_pages,
+                               uint8_t *k_scales, uint8_t *v_scales, void *stream);
+
+/*
+ * Read cached rows back: k, v [n_tokens][n_kv_heads][head_dim] (bfloat16, contiguous) receive the values
+ * that the packed tokens' positions hold (token i of sequence b: position pos[b] + i), bit for bit what the
+ * attention works with: a cached prefix for pbb_prefill or another cache.  Tokens whose position has no
+ * page, and those of skipped sequences, become zeros; rows before q_start[0] or from q_start[batch] on are
+ * left as they are.
+ */
+pbb_status_t pbb_coded_read(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
+                             const int32_t *q_start, const int32_t *table, const void *k_pages,
+                             const void *v_pages, const uint8_t *k_scales, const uint8_t *v_scales,
+                             void *k, void *v, void *stream);
+
+/*
+ * Attention of the packed tokens over the 8-bit cache: pbb_paged_attention of the values that codes and
+ * scales stand for, with its supports, masks, empty supports and log-partitions.  Scores are products of the
+ * unquantised queries (rows of q down to 2^-22 of their largest magnitude) with fp32 accumulation; the
+ * value products take weights as pbb_paged_attention does.  workspace: pbb_coded_workspace_bytes bytes,
+ * by the rules of pbb_paged_workspace_bytes (its first PBB_PAGED_COUNTER_BYTES zero before the first call, and
+ * left zero).
+ */
+pbb_status_t pbb_coded_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_tokens, size_t *bytes);
+
+pbb_status_t pbb_coded_attention(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
+                                  const int32_t *q_start, const int32_t *table, const void *q,
+                                  int64_t q_stride, const void *k_pages, const void *v_pages,
+                                  const uint8_t *k_scales, const uint8_t *v_scales, void *out, float *lse,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

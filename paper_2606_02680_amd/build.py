@@ -3,7 +3,8 @@
 ``python -m paper_2606_02680_amd.build`` compiles ``csrc/pbb_api.cpp``,
 ``csrc/pbb_kernels.hip`` (decode), ``csrc/pbb_prefill.hip`` (prefill),
 ``csrc/pbb_backward.hip`` (training backward), ``csrc/pbb_paged_api.cpp``, ``csrc/pbb_rotary.hip``
-(rotary rows, paged append) and ``csrc/pbb_paged*.hip`` (attention over a paged cache) into ``paper_2606_02680_amd/libpbb.so`` (and the
+(rotary rows, paged append), ``csrc/pbb_paged*.hip`` (attention over a paged cache, and the 8-bit one
+with its rows) and ``csrc/pbb_norm*`` (norms with rotation) into ``paper_2606_02680_amd/libpbb.so`` (and the
 streaming-read probe ``csrc/pbb_probe.hip``, a measurement helper, into ``libpbbprobe.so``) and
 writes the compiler's
 per-kernel resource report (VGPRs, AGPRs, SGPRs, LDS, scratch) to ``_build/resource_usage.txt``
@@ -23,7 +24,8 @@ PROBE_LIB = os.path.join(PKG, "libpbbprobe.so")   # measurement helper (include/
 ARCH = "gfx950"
 
 SOURCES = ("pbb_api.cpp", "pbb_kernels.hip", "pbb_prefill.hip", "pbb_backward.hip",
-           "pbb_paged_api.cpp", "pbb_rotary.hip", "pbb_paged.hip", "pbb_paged_f32.hip")
+           "pbb_paged_api.cpp", "pbb_rotary.hip", "pbb_paged.hip", "pbb_paged_f32.hip",
+           "pbb_norm_api.cpp", "pbb_norm.hip", "pbb_coded_api.cpp", "pbb_coded_rows.hip", "pbb_coded.hip")
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,256 @@
+// Appending to an 8-bit paged cache, and reading it back, on gfx950 (MI355X).
+//
+// The append takes a chunk's new keys through the norm and the rotation (pbb_norm.hip has the formulas),
+// all in fp32, and rounds once, to e4m3 codes under the row's power of two (pbb_coded_device.h); values
+// are quantised as they come, queries go out as bf16 rows.  Reading back is exact: a code times a power
+// of two is a bf16 value.
+//
+// Bound: HBM (each row read once and written once), small calls by the launch.  Append: a lane takes 8
+// channels and their partners d/2 further on, as in the rotation, and writes 8 codes of each half.  Read:
+// a lane takes 16 codes and writes 32 bytes.
+
+#include "pbb_norm_internal.h"
+#include "pbb_coded_device.h"
+#include "pbb_rows.h"
+
+namespace pbb {
+namespace {
+
+// The sequence that packed row `tok` belongs to, or -1, where the lanes of a wave may have tokens of their
+// own from `first` (the wave's lowest) to `last`.
+__device__ __forceinline__ int lane_sequence(const int32_t* q_start, int batch, int tok, int first, int last,
+                                             int lane) {
+  int b = count_upto(q_start + 1, batch, first, lane);   // sequences that end at or before the first
+  if (b < batch && __builtin_amdgcn_readfirstlane(q_start[b + 1]) <= last) {
+    int lo = b, n = batch - b;   // the others of the wave: a search each
+    while (n > 0) {
+      const int half = n >> 1;
+      const bool up = q_start[lo + half + 1] <= tok;
+      lo = up ? lo + half + 1 : lo;
+      n = up ? n - half - 1 : half;
+    }
+    b = lo;
+  }
+  return b < batch && q_start[b] <= tok ? b : -1;
+}
+
+// What a packed token is: its sequence (-1: none), position, and its row in the pool under KV head 0 (-1:
+// no page holds its position); consecutive heads' rows are page_size apart.
+struct Place {
+  int b, t;
+  bool skip;
+  int64_t row;
+};
+template <typename A>
+__device__ __forceinline__ Place place_of(const A& a, int tok, int first, int last, int lane) {
+  Place p;
+  p.b = a.uniform >= 0 ? a.by_uniform.div(tok) : lane_sequence(a.q_start, a.batch, tok, first, last, lane);
+  p.t = 0;
+  p.skip = true;
+  p.row = -1;
+  if (p.b < 0) return p;
+  const Chunk c = chunk_of(p.b, a.uniform, a.uniform >= 0 ? 0 : a.q_start[p.b],
+                           a.uniform >= 0 ? 0 : a.q_start[p.b + 1], a.pos[p.b], a.n);
+  p.skip = c.pos < 0;
+  p.t = p.skip ? 0 : c.pos + (tok - c.row0);
+  if (!p.skip && p.t < a.shape.capacity) {
+    const int i = a.shape.by_page.div(p.t);
+    const int id = a.table[(size_t)p.b * a.shape.width + i];
+    if (a.shape.is_page(id))
+      p.row = (int64_t)id * a.hkv * a.shape.page_size + (p.t - i * a.shape.page_size);
+  }
+  return p;
+}
+
+template <int PC>
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {   // over the PC (4 or 8) adjacent lanes of a row
+  auto step = [](uint32_t v, uint32_t o) { return v > o ? v : o; };
+  x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true));
+  x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true));
+  if constexpr (PC >= 8) x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));
+  return x;
+}
+template <int PC>
+__device__ __forceinline__ float row_sum(float x) {
+  auto from = [](float v, auto ctrl) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v),
+                                                                 decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x += from(x, std::integral_constant<int, 0xB1>{});
+  x += from(x, std::integral_constant<int, 0x4E>{});
+  if constexpr (PC >= 8) x += from(x, std::integral_constant<int, 0x141>{});
+  return x;
+}
+
+// Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's query rows, key rows and
+// value rows (in this order).
+template <int D>
+__global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendArgs a) {
+  typedef uint16_t T;
+  constexpr int N = Piece<T>::N;
+  constexpr int ROWB = D * 2;
+  constexpr int PC = ROWB / 32;
+  constexpr int ROWS = 64 / PC;
+  const int lane = threadIdx.x & 63;
+  const int tpw = a.tokens_per_wave;
+  const int64_t first = ((int64_t)token_group() * (kRotThreads / 64) +
+                         __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * tpw;
+  if (first >= a.n) return;
+  const int hq = a.q != nullptr ? a.hq : 0;
+  const int rows = hq + 2 * a.hkv;
+  const int sub = tpw > 1 ? a.by_rows.div(lane / PC) : 0;
+  const int last = min((int)first + tpw - 1, a.n - 1);
+  const int tok = min((int)first + sub, last);
+  const Place at = place_of(a, tok, (int)first, last, lane);
+  if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
+  const int pc = lane % PC;
+  float cs[N], sn[N];
+  if (a.turn)
+    piece_turns<T>(a.rope, pc,
+                   [&](int axis) {
+                     return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : at.t;
+                   },
+                   cs, sn);
+  const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
+  for (int r = blockIdx.y * a.run + lane / PC - sub * rows; r < r1; r += ROWS) {
+    const bool query = r < hq, value = r >= hq + a.hkv;
+    const unsigned char* src =
+        (query ? (const unsigned char*)a.q + tok * a.q_stride + (size_t)r * ROWB
+         : !value ? (const unsigned char*)a.k + tok * a.k_stride + (size_t)(r - hq) * ROWB
+                  : (const unsigned char*)a.v + tok * a.v_stride + (size_t)(r - hq - a.hkv) * ROWB) + pc * 16;
+    const u32x4 lo = *(const u32x4*)src, hi = *(const u32x4*)(src + ROWB / 2);
+    float y[N], z[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = Piece<T>::get(lo, e), z[e] = Piece<T>::get(hi, e);
+    if (a.norm && !value) {
+      const unsigned char* wp = (const unsigned char*)(query ? a.q_weight : a.k_weight);
+      float ss = 0.0f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) ss = __builtin_fmaf(y[e], y[e], __builtin_fmaf(z[e], z[e], ss));
+      const float rs = 1.0f / __builtin_sqrtf(__builtin_fmaf(row_sum<PC>(ss), 1.0f / D, a.eps));
+      if (wp != nullptr) {
+        const u32x4 wl = *(const u32x4*)(wp + pc * 16), wh = *(const u32x4*)(wp + ROWB / 2 + pc * 16);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          y[e] = y[e] * rs * Piece<T>::get(wl, e);
+          z[e] = z[e] * rs * Piece<T>::get(wh, e);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] *= rs, z[e] *= rs;
+      }
+    }
+    if (a.turn && !value) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float s = y[e], t = z[e];
+        rope_turn(s, t, cs[e], sn[e], y[e], z[e]);
+      }
+    }
+    if (query) {
+      unsigned char* w = (unsigned char*)a.q_out + ((size_t)tok * hq + r) * ROWB + pc * 16;
+      const u32x4 none = {0u, 0u, 0u, 0u};
+      *(u32x4*)w = at.skip ? none : Piece<T>::put(y);
+      *(u32x4*)(w + ROWB / 2) = at.skip ? none : Piece<T>::put(z);
+      continue;
+    }
+    if (at.row < 0) break;   // (the rows after it are keys and values too)
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t u = finite_bits(y[e]), v = finite_bits(z[e]);
+      most = u > most ? u : most;
+      most = v > most ? v : most;
+    }
+    const int ex = scale_exponent(row_max<PC>(most), kScaleHi);
+    const float inv = power_of_two(-ex);
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] *= inv, z[e] *= inv;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(ex == kScaleHi) != 0, 0)) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[e] = cut_finite(y[e]), z[e] = cut_finite(z[e]);
+    }
+    const int h = r - hq - (value ? a.hkv : 0);
+    const int64_t row = at.row + (int64_t)h * a.shape.page_size;
+    uint8_t* w = (value ? a.v_pages : a.k_pages) + row * D + pc * 8;
+    *(u32x2*)w = u32x2{codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7])};
+    *(u32x2*)(w + D / 2) = u32x2{codes4(z[0], z[1], z[2], z[3]), codes4(z[4], z[5], z[6], z[7])};
+    if (pc == 0) (value ? a.v_scales : a.k_scales)[row] = (uint8_t)(ex + 127);
+  }
+}
+
+// Grid as the append's, over a token's key rows and value rows.
+template <int D>
+__global__ __launch_bounds__(kRotThreads) void coded_read_kernel(CodedReadArgs a) {
+  constexpr int PC = D / 16;
+  constexpr int ROWS = 64 / PC;
+  constexpr int ROWB = D * 2;
+  const int lane = threadIdx.x & 63;
+  const int tpw = a.tokens_per_wave;
+  const int64_t first = ((int64_t)token_group() * (kRotThreads / 64) +
+                         __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * tpw;
+  if (first >= a.n) return;
+  const int rows = 2 * a.hkv;
+  const int sub = tpw > 1 ? a.by_rows.div(lane / PC) : 0;
+  const int last = min((int)first + tpw - 1, a.n - 1);
+  const int tok = min((int)first + sub, last);
+  const Place at = place_of(a, tok, (int)first, last, lane);
+  if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
+  const int pc = lane % PC;
+  const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
+  for (int r = blockIdx.y * a.run + lane / PC - sub * rows; r < r1; r += ROWS) {
+    const bool value = r >= a.hkv;
+    const int h = r - (value ? a.hkv : 0);
+    u32x4 w = {0u, 0u, 0u, 0u};
+    float scale = 1.0f;
+    if (at.row >= 0) {
+      const int64_t row = at.row + (int64_t)h * a.shape.page_size;
+      w = *(const u32x4*)((value ? a.v_pages : a.k_pages) + row * D + pc * 16);
+      scale = power_of_two((int)(value ? a.v_scales : a.k_scales)[row] - 127);
+    }
+    unsigned char* o = (unsigned char*)(value ? a.v : a.k) + ((size_t)tok * a.hkv + h) * ROWB + pc * 32;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *(u32x4*)(o + 16 * i) = u32x4{values2<false>(w[2 * i], scale), values2<true>(w[2 * i], scale),
+                                    values2<false>(w[2 * i + 1], scale), values2<true>(w[2 * i + 1], scale)};
+  }
+}
+
+// Sets the launcher's fields; returns the grid.
+template <typename A>
+dim3 rows_grid(A& a, int rows, int per_pass) {
+  constexpr int WAVES = kRotThreads / 64;
+  a.tokens_per_wave = rows < per_pass ? per_pass / rows : 1;
+  a.run = rows < per_pass ? rows : head_run(a.n, rows, per_pass);
+  a.by_rows = FastDiv::make((uint32_t)rows);
+  const int per = WAVES * a.tokens_per_wave;
+  return token_grid(((int64_t)a.n + per - 1) / per, (rows + a.run - 1) / a.run);
+}
+
+template <int D>
+hipError_t append_t(const CodedAppendArgs& a0, hipStream_t stream) {
+  CodedAppendArgs a = a0;
+  const dim3 grid = rows_grid(a, (a.q != nullptr ? a.hq : 0) + 2 * a.hkv, 64 / (D / 16));
+  hipLaunchKernelGGL((coded_append_kernel<D>), grid, dim3(kRotThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t read_t(const CodedReadArgs& a0, hipStream_t stream) {
+  CodedReadArgs a = a0;
+  const dim3 grid = rows_grid(a, 2 * a.hkv, 64 / (D / 16));
+  hipLaunchKernelGGL((coded_read_kernel<D>), grid, dim3(kRotThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_coded_append(const CodedAppendArgs& a, int32_t head_dim, hipStream_t stream) {
+  return head_dim == 64 ? append_t<64>(a, stream) : append_t<128>(a, stream);
+}
+
+hipError_t launch_coded_read(const CodedReadArgs& a, int32_t head_dim, hipStream_t stream) {
+  return head_dim == 64 ? read_t<64>(a, stream) : read_t<128>(a, stream);
+}
+
+}  // namespace pbb

@@ -1,0 +1,124 @@
+// Internal interface between the C-ABI layer (pbb_norm_api.cpp, pbb_coded_api.cpp) and the HIP kernels of
+// the norms with rotation (pbb_norm.hip) and of the 8-bit paged cache (pbb_coded_rows.hip,
+// pbb_coded.hip).  Not installed; not part of the public ABI.
+#pragma once
+
+#include "pbb_paged_internal.h"
+
+namespace pbb {
+
+// Rows of one kind (queries or keys) of a norm call.  Strides in bytes.
+struct NormPart {
+  const void* x;
+  const void* grad;      // backward: the gradient of the rotated rows
+  void* out;             // forward: the rotated rows; backward: the gradient of x
+  const void* weight;    // [head_dim], null: ones
+  float* dweight;        // backward, optional: [head_dim]
+  int64_t x_stride, grad_stride, out_stride;
+  int32_t heads;         // 0: no rows of this kind
+  // set by the launcher
+  int32_t run;           // heads of a unit of work, and units per group of tokens
+  int32_t tokens_per_wave;
+  int32_t units;
+  int32_t blocks;        // workgroups
+  FastDiv by_heads, by_runs;
+};
+
+// Norm and rotation of rows, validated on the host; n >= 1 (backward: >= 0).
+struct NormArgs {
+  NormPart part[2];            // queries, keys
+  const int32_t* positions;    // [axes][n]
+  float* partials;             // backward: partial sums of the weights' gradients
+  int32_t n;
+  int32_t turn;                // 1: rope applies
+  float eps;
+  RopeArgs rope;               // negative rates turn backwards
+};
+
+// Workgroups of a backward launch, both kinds together, at most: four per CU, each with one partial sum
+// of a weight's gradient.
+constexpr int kNormBlocks = 1024;
+constexpr int kNormThreads = 256;
+
+// Tokens that a wave of `rows` rows at a time takes together, and a backward launch's workgroups of a
+// kind of `heads` of `all` heads.
+inline int norm_tokens_per_wave(int heads, int rows) { return heads < rows ? rows / heads : 1; }
+inline int norm_grad_blocks(int n, int heads, int all, int rows) {
+  if (heads == 0) return 0;
+  const int64_t per = (int64_t)(kNormThreads / 64) * norm_tokens_per_wave(heads, rows);
+  const int64_t most = (n + per - 1) / per;
+  const int64_t share = (int64_t)kNormBlocks * heads / all;
+  const int64_t b = share < 1 ? 1 : share;
+  return (int)(b < most ? b : most);
+}
+
+// Rows of the 8-bit paged cache, validated on the host; n >= 1.  Strides in bytes.
+struct CodedAppendArgs {
+  const int32_t* pos;
+  const int32_t* q_start;     // null with uniform >= 0
+  const int32_t* table;
+  const int32_t* rope_pos;    // null: the cache position
+  const void* q;              // null: no queries
+  void* q_out;
+  const void* k;
+  const void* v;
+  const void* q_weight;       // null: ones
+  const void* k_weight;
+  uint8_t* k_pages;           // [n_pages][hkv][page_size][d] codes
+  uint8_t* v_pages;
+  uint8_t* k_scales;          // [n_pages][hkv][page_size] scale bytes
+  uint8_t* v_scales;
+  int64_t q_stride, k_stride, v_stride;
+  int32_t n;
+  int32_t batch;
+  int32_t uniform;            // tokens of every sequence, -1: q_start says
+  int32_t hq;
+  int32_t hkv;
+  int32_t turn;               // 1: rope applies
+  int32_t norm;               // 1: the norms apply
+  float eps;
+  int32_t run;                // rows per grid row (this and the next two set by the launcher)
+  int32_t tokens_per_wave;
+  FastDiv by_rows;
+  FastDiv by_uniform;
+  PagedShape shape;
+  RopeArgs rope;
+};
+
+struct CodedReadArgs {
+  const int32_t* pos;
+  const int32_t* q_start;
+  const int32_t* table;
+  const uint8_t* k_pages;
+  const uint8_t* v_pages;
+  const uint8_t* k_scales;
+  const uint8_t* v_scales;
+  void* k;                    // [n][hkv][d]
+  void* v;
+  int32_t n;
+  int32_t batch;
+  int32_t uniform;
+  int32_t hkv;
+  int32_t run;                // (this and the next two set by the launcher)
+  int32_t tokens_per_wave;
+  FastDiv by_rows;
+  FastDiv by_uniform;
+  PagedShape shape;
+};
+
+// Attention over an 8-bit paged cache, validated on the host; n >= 1.  p.k_pages and p.v_pages hold codes.
+struct CodedArgs {
+  PagedArgs p;
+  const uint8_t* k_scales;
+  const uint8_t* v_scales;
+};
+
+inline PagedKind coded_kind(bool narrow, int head_dim) { return paged_kind(false, narrow, head_dim); }
+
+hipError_t launch_norm_rotate(const NormArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
+hipError_t launch_norm_rotate_backward(const NormArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
+hipError_t launch_coded_append(const CodedAppendArgs& a, int32_t head_dim, hipStream_t stream);
+hipError_t launch_coded_read(const CodedReadArgs& a, int32_t head_dim, hipStream_t stream);
+hipError_t launch_coded_attention(const CodedArgs& a, int32_t head_dim, hipStream_t stream);
+
+}  // namespace pbb

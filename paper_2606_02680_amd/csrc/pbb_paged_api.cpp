@@ -6,112 +6,20 @@
 
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-#include <cstdint>
-
-#include "pbb_paged_internal.h"
+#include "pbb_checks.h"
 
 namespace {
+
+using namespace pbb_checks;
 
 static_assert(PBB_PAGED_COUNTER_BYTES == pbb::kPagedCounterBytes, "counter block");
 static_assert((2 * pbb::kPagedMaxPieces + pbb::kPagedMaxPieces / 8 + pbb::kPagedMaxPieces) * 4 <=
                   (int)pbb::kPagedCounterBytes,
               "a counter per partial state (2 more per head, of at most kPagedMaxPieces / 2 heads)");
 
-constexpr int32_t kMaxTokens = 1 << 30;
-constexpr int32_t kMaxCapacity = 1 << 30;
-constexpr int32_t kMaxBatch = 1 << 24;
-// Tiles of an attention call in all heads.  With the pieces (some 2176) and one workgroup per head (at
-// most 2^18) more, a launch of 256 threads each stays below 2^32 threads.
-constexpr uint64_t kMaxTiles = 1u << 23;
-constexpr int32_t kMaxPage = 1 << 20;   // (a page's rows under one KV head lie within 32-bit byte offsets)
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-int64_t elem_bytes(int32_t dtype) { return dtype == PBB_DTYPE_F32 ? 4 : 2; }
-
-bool known_dtype(int32_t dtype) { return dtype == PBB_DTYPE_F32 || dtype == PBB_DTYPE_BF16; }
-
-pbb_status_t check_rope(const pbb_rope_t* r, int32_t head_dim) {
-  if (r->head_dim != head_dim) return PBB_ERR_SHAPE;
-  if (r->n_axes < 1 || r->n_axes > PBB_MAX_AXES) return PBB_ERR_SHAPE;
-  for (int c = 0; c < head_dim / 2; ++c)   // (below 2^992 no position's turns pass the largest double)
-    if (r->axis[c] >= r->n_axes || !(std::fabs(r->turns[c]) < 0x1p992)) return PBB_ERR_SHAPE;
-  return PBB_OK;
-}
-
-pbb::RopeArgs rope_args(const pbb_rope_t* r, double sign) {
-  pbb::RopeArgs a;
-  for (int c = 0; c < 64; ++c) {
-    const bool used = r != nullptr && c < r->head_dim / 2;
-    a.turns[c] = used ? sign * r->turns[c] : 0.0;
-    a.axis[c] = used ? r->axis[c] : 0;
-  }
-  return a;
-}
-
-// Token stride of rows [n][heads][d] in elements: room for a token's rows, whole 16-byte pieces,
-// and no byte offset beyond 2^62.
-bool stride_ok(int64_t stride, int64_t heads, int64_t d, int64_t u) {
-  return stride >= heads * d && (stride * u) % 16 == 0 && stride < (int64_t(1) << 28);
-}
-
-pbb_status_t check_paged(const pbb_paged_desc_t* d, int32_t n) {
-  if (d == nullptr) return PBB_ERR_NULL;
-  if (!known_dtype(d->dtype)) return PBB_ERR_DTYPE;
-  if (d->batch < 1 || d->batch > kMaxBatch || d->n_kv_heads < 1 || d->n_q_heads < 1) return PBB_ERR_SHAPE;
-  if (d->n_q_heads % d->n_kv_heads != 0) return PBB_ERR_SHAPE;
-  if (d->n_q_heads / d->n_kv_heads > pbb::kMaxGroup) return PBB_ERR_SHAPE;
-  if (d->head_dim != 64 && d->head_dim != 128) return PBB_ERR_SHAPE;
-  if ((int64_t)d->n_q_heads * d->head_dim > (1 << 24)) return PBB_ERR_SHAPE;
-  if (d->page_size < 16 || d->page_size > kMaxPage || d->page_size % 16 != 0) return PBB_ERR_SHAPE;
-  if (d->n_pages < 1 || d->table_width < 1) return PBB_ERR_SHAPE;
-  if ((int64_t)d->page_size * d->table_width > kMaxCapacity) return PBB_ERR_SHAPE;
-  if (d->block < 0 || d->block % 2 != 0 || d->window < 0 || (d->block > 0 && d->window > 0))
-    return PBB_ERR_SHAPE;
-  if (n < 0 || n > kMaxTokens) return PBB_ERR_SHAPE;
-  if ((int64_t)d->batch * d->table_width >= (int64_t(1) << 40) ||
-      (int64_t)d->n_q_heads * n >= (int64_t(1) << 40))
-    return PBB_ERR_SHAPE;
-  return PBB_OK;
-}
-
-pbb::PagedShape shape_of(const pbb_paged_desc_t* d) {
-  return pbb::PagedShape::make(d->page_size, d->n_pages, d->table_width, d->block, d->window);
-}
-
-pbb::PagedPlan plan_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s, int32_t n, bool ragged) {
-  const int group = d->n_q_heads / d->n_kv_heads;
-  const bool narrow = pbb::PagedPlan::is_narrow(d->batch, group, n, ragged);
-  return pbb::PagedPlan::make(s, pbb::paged_kind(d->dtype == PBB_DTYPE_F32, narrow, d->head_dim),
-                              d->batch, d->n_kv_heads, group, n, ragged);
-}
-
-size_t states_of(const pbb_paged_desc_t* d, const pbb::PagedPlan& p) {
-  return (size_t)p.slots * d->n_kv_heads * pbb::paged_state_bytes(p.cols, d->head_dim);
-}
-
-// What any call may need: calls of few columns per sequence are all planned alike, of the others one of
-// a single token needs most (which of them a call is, its q_start decides).  So the size depends on the
-// descriptor alone.
-struct Workspace {   // counters, `states` bytes of partial states, the sequences' summary
-  size_t bytes, states;
-};
-Workspace workspace_of(const pbb_paged_desc_t* d, const pbb::PagedShape& s) {
-  const int group = d->n_q_heads / d->n_kv_heads;
-  const bool f32 = d->dtype == PBB_DTYPE_F32;
-  const size_t narrow = states_of(
-      d, pbb::PagedPlan::make(s, pbb::paged_kind(f32, true, d->head_dim), d->batch, d->n_kv_heads, group,
-                              d->batch, false));
-  const size_t wide = states_of(
-      d, pbb::PagedPlan::make(s, pbb::paged_kind(f32, false, d->head_dim), d->batch, d->n_kv_heads, group,
-                              1, true));
-  Workspace w;
-  w.states = narrow > wide ? narrow : wide;
-  const int scanned = w.states > 0 ? pbb::kPagedScan : pbb::kPagedScanUncut;   // (PagedPlan::planned)
-  const size_t bytes = w.states + (d->batch > scanned ? (size_t)pbb::paged_rounds_bytes(d->batch) : 0);
-  w.bytes = bytes > 0 ? pbb::kPagedCounterBytes + bytes : 0;
-  return w;
+// The rules of a descriptor's attention kernels.
+auto kind_of(const pbb_paged_desc_t* d) {
+  return [d](bool narrow) { return pbb::paged_kind(d->dtype == PBB_DTYPE_F32, narrow, d->head_dim); };
 }
 
 }  // namespace
@@ -232,7 +140,7 @@ pbb_status_t pbb_paged_workspace_bytes(const pbb_paged_desc_t* desc, int32_t n_t
   if (desc == nullptr || bytes == nullptr) return PBB_ERR_NULL;
   const pbb_status_t st = check_paged(desc, n_tokens);
   if (st != PBB_OK) return st;
-  *bytes = workspace_of(desc, shape_of(desc)).bytes;
+  *bytes = workspace_of(desc, shape_of(desc), kind_of(desc)).bytes;
   return PBB_OK;
 }
 
@@ -249,24 +157,17 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   if (n_tokens == 0) return PBB_OK;
   pbb::PagedArgs a;
   a.shape = shape_of(desc);
-  a.plan = plan_of(desc, a.shape, n_tokens, q_start != nullptr);
+  a.plan = plan_of(desc, a.shape, n_tokens, q_start != nullptr, kind_of(desc));
   if ((uint64_t)a.plan.tiles * (uint64_t)desc->n_kv_heads > kMaxTiles) return PBB_ERR_SHAPE;
   if (!pos || !table || !q || !k_pages || !v_pages || !out) return PBB_ERR_NULL;
   if (!aligned(pos, 4) || !aligned(q_start, 4) || !aligned(table, 4) || !aligned(q, 16) ||
       !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) || !aligned(lse, 4))
     return PBB_ERR_ALIGN;
-  const Workspace ws = workspace_of(desc, a.shape);
-  const size_t own = ws.states + (a.plan.planned ? (size_t)pbb::paged_rounds_bytes(desc->batch) : 0);
-  const size_t need = own > 0 ? pbb::kPagedCounterBytes + own : 0;
+  const Workspace ws = workspace_of(desc, a.shape, kind_of(desc));
+  const size_t need = workspace_need(desc, a.plan, ws);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return PBB_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return PBB_ERR_ALIGN;
-  a.counters = need > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
-  a.states = need > 0 ? reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) +
-                                                 pbb::kPagedCounterBytes)
-                      : nullptr;
-  a.rounds = need > 0 ? reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) +
-                                                    pbb::kPagedCounterBytes + ws.states)
-                      : nullptr;
+  take_workspace(a, need, ws, workspace);
   a.pos = pos;
   a.q_start = q_start;
   a.table = table;
@@ -281,9 +182,7 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t* desc, int32_t n_tokens,
   a.hq = desc->n_q_heads;
   a.hkv = desc->n_kv_heads;
   a.group = desc->n_q_heads / desc->n_kv_heads;
-  const float scale = desc->scale > 0.0f ? desc->scale
-                                         : (float)(1.0 / std::sqrt((double)desc->head_dim));
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);  // log2(e)
+  a.scale_log2 = scale_log2(desc);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = a.plan.planned ? pbb::launch_paged_plan(a, s) : hipSuccess;
   if (e == hipSuccess)

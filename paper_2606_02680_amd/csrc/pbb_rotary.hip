@@ -10,89 +10,10 @@
 // half row), so a wave reads 64 / PC whole rows at once and works out its sines and cosines once for
 // all rows of the token that it visits.
 
-#include "pbb_device.h"
-#include "pbb_paged_device.h"
+#include "pbb_rows.h"
 
 namespace pbb {
 namespace {
-
-constexpr int kRotThreads = 256;
-// A grid's x has fewer than 2^32 threads: groups of tokens beyond kGridX go on along z.
-constexpr int kGridX = 1 << 23;
-__device__ __forceinline__ int token_group() { return (int)(blockIdx.z * kGridX + blockIdx.x); }
-dim3 token_grid(int64_t groups, int runs) {
-  return dim3((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)runs,
-              (unsigned)((groups + kGridX - 1) / kGridX));
-}
-// Rows of more bytes than the last-level cache (256 MB) are read and written with the non-temporal
-// hint: what is written first is gone before anything reads it (4 x 16384 tokens of 32 heads, d 128:
-// 537 MB, 259 us with the 8 key heads' call, 239 to 241 with the hint, 5.6 TB/s; 16000 tokens, 131 MB: the
-// next kernel finds them in the cache).
-constexpr int64_t kStreamBytes = 256ll << 20;
-
-template <typename T>
-struct Piece;   // 16 bytes of a row as floats
-template <>
-struct Piece<uint16_t> {
-  static constexpr int N = 8;
-  typedef u32x4 raw;
-  static __device__ __forceinline__ float get(raw r, int e) {
-    return __uint_as_float(e & 1 ? r[e >> 1] & 0xFFFF0000u : r[e >> 1] << 16);
-  }
-  static __device__ __forceinline__ raw put(const float (&f)[N]) {
-    return raw{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]),
-               pack_bf16(f[6], f[7])};
-  }
-};
-template <>
-struct Piece<float> {
-  static constexpr int N = 4;
-  typedef u32x4 raw;
-  static __device__ __forceinline__ float get(raw r, int e) { return __uint_as_float(r[e]); }
-  static __device__ __forceinline__ raw put(const float (&f)[N]) {
-    return raw{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
-               __float_as_uint(f[3])};
-  }
-};
-
-// cos and sin of `turns` whole turns.  The angle is reduced to half a turn either way in fp64.
-// bf16: the hardware's sine and cosine (of turns; their error of a few 2^-22 is far below the
-// rounding of the result); fp32: sincospif, whose last-bit error is of the order of the result's.
-template <typename T>
-__device__ __forceinline__ void cos_sin(double turns, float& cs, float& sn) {
-  const float f = (float)(turns - __builtin_rint(turns));
-  if constexpr (sizeof(T) == 2) {
-    cs = __builtin_amdgcn_cosf(f);
-    sn = __builtin_amdgcn_sinf(f);
-  } else {
-    sincospif(2.0f * f, &sn, &cs);
-  }
-}
-
-// The sines and cosines of piece pc of a row (pairs pc N .. + N - 1) at a token's positions;
-// position(axis) reads them.
-template <typename T, typename F>
-__device__ __forceinline__ void piece_turns(const RopeArgs& r, int pc, F&& position,
-                                            float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
-  constexpr int N = Piece<T>::N;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int c = pc * N + e;
-    cos_sin<T>((double)position(r.axis[c]) * r.turns[c], cs[e], sn[e]);
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&cs)[Piece<T>::N],
-                                            const float (&sn)[Piece<T>::N]) {
-  constexpr int N = Piece<T>::N;
-  float ox[N], oy[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    rope_turn(Piece<T>::get(lo, e), Piece<T>::get(hi, e), cs[e], sn[e], ox[e], oy[e]);
-  lo = Piece<T>::put(ox);
-  hi = Piece<T>::put(oy);
-}
 
 // Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's heads.  Where a token
 // has fewer heads than a wave takes rows, a wave takes several tokens (2 heads, d 64, 16000 tokens with
@@ -130,14 +51,6 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
       *(u32x4*)(w + ROWB / 2) = hi;
     }
   }
-}
-
-// The sequence that packed row `tok` belongs to, or -1: the number of sequences whose rows end at or
-// before it (every lane of the wave takes part; q_start never falls).
-__device__ __forceinline__ int sequence_of(const int32_t* q_start, int batch, int tok, int lane) {
-  const int b = count_upto(q_start + 1, batch, tok, lane);
-  if (b >= batch) return -1;
-  return __builtin_amdgcn_readfirstlane(q_start[b]) <= tok ? b : -1;
 }
 
 // Grid as rotate_kernel, over a token's query rows, key rows and value rows (in this order).
@@ -211,15 +124,6 @@ __global__ __launch_bounds__(kRotThreads) void paged_append_kernel(AppendArgs a)
       *(u32x4*)(w + pc * 16 + ROWB / 2) = hi[u];
     }
   }
-}
-
-// Heads per workgroup row of the grid: all of a token's, unless the tokens alone leave the chip
-// short of waves; then as few as a wave takes at once, and no more than 65535 runs (2000 tokens of 48
-// rows: 11.5 us, 13.5 with a run per 8 rows; 256 tokens: 5.0 us so; inputs in the last-level cache).
-int head_run(int tokens, int heads, int rows) {
-  if (tokens >= 1024) return heads;
-  const int least = (heads + 65534) / 65535;
-  return rows > least ? rows : least;
 }
 
 template <typename T, int D>

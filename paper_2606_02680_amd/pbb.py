@@ -26,7 +26,9 @@ EXPORTS = ("pbb_status_string", "pbb_ring_bytes", "pbb_ring_init", "pbb_ring_fil
            "pbb_decode_step_advance", "swa_decode_step_advance", "pbb_prefill", "swa_prefill",
            "pbb_backward_workspace_bytes", "pbb_backward", "swa_backward",
            "pbb_decode_step_noalloc", "pbb_rope_init", "pbb_rotate", "pbb_paged_append",
-           "pbb_paged_workspace_bytes", "pbb_paged_attention")
+           "pbb_paged_workspace_bytes", "pbb_paged_attention", "pbb_norm_rotate",
+           "pbb_norm_workspace_bytes", "pbb_norm_rotate_backward", "pbb_coded_append",
+           "pbb_coded_read", "pbb_coded_workspace_bytes", "pbb_coded_attention")
 
 
 class PbbError(RuntimeError):
@@ -56,6 +58,11 @@ class PbbRope(ctypes.Structure):
     """Mirror of ``pbb_rope_t``."""
     _fields_ = [("head_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
                 ("turns", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class PbbNorm(ctypes.Structure):
+    """Mirror of ``pbb_norm_t``."""
+    _fields_ = [("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
 
 
 class PbbPagedDesc(ctypes.Structure):
@@ -109,6 +116,17 @@ def load_library(path: str = _LIB_PATH):
                                      vp, vp]
     lib.pbb_paged_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
     lib.pbb_paged_attention.argtypes = [pp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    np = ctypes.POINTER(PbbNorm)
+    lib.pbb_norm_rotate.argtypes = [np, rp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, i64,
+                                    i32, vp]
+    lib.pbb_norm_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.pbb_norm_rotate_backward.argtypes = [np, rp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64,
+                                             vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]
+    lib.pbb_coded_append.argtypes = [pp, i32, vp, vp, vp, np, rp, vp, vp, i64, vp, vp, i64, vp, i64, vp,
+                                      vp, vp, vp, vp]
+    lib.pbb_coded_read.argtypes = [pp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.pbb_coded_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
+    lib.pbb_coded_attention.argtypes = [pp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     for fn in EXPORTS[1:]:
         getattr(lib, fn).restype = ctypes.c_int
     _lib = lib
@@ -493,6 +511,14 @@ def make_paged_desc(batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, 
                         window, int(code), float(scale))
 
 
+def _workspace_size(workspace, device: int) -> int:
+    """Bytes of a caller's workspace."""
+    _expect_on("workspace", workspace, device)
+    if not workspace.is_contiguous():   # (its bytes would not be numel of them, one after another)
+        raise ValueError("workspace: must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
 def pages_shape(desc: PbbPagedDesc):
     return (desc.n_pages, desc.n_kv_heads, desc.page_size, desc.head_dim)
 
@@ -513,16 +539,19 @@ def paged_workspace_bytes(desc: PbbPagedDesc, n_tokens: int) -> int:
 PAGED_COUNTER_BYTES = 65536
 
 
+def _counted_workspace(nbytes: int, device):
+    if nbytes == 0:
+        return None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    ws[:PAGED_COUNTER_BYTES].zero_()
+    return ws
+
+
 def alloc_paged_workspace(desc: PbbPagedDesc, n_tokens: int, device="cuda"):
     """Workspace for :func:`pbb_paged_attention` calls with ``desc``, its counters zero, or None when they
     need none; the same for every ``n_tokens``.  Calls leave the counters zero, so one allocation
     serves every later call on one stream (calls that may overlap need their own)."""
-    n = paged_workspace_bytes(desc, n_tokens)
-    if n == 0:
-        return None
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
-    ws[:PAGED_COUNTER_BYTES].zero_()
-    return ws
+    return _counted_workspace(paged_workspace_bytes(desc, n_tokens), device)
 
 
 def _expect_paged(desc: PbbPagedDesc, pos, table, q_start, k_pages, v_pages, dev: int):
@@ -581,10 +610,7 @@ def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out
         _dense("lse", lse, (hq, n), torch.float32, dev)
     ws_bytes = 0
     if workspace is not None:
-        _expect_on("workspace", workspace, dev)
-        if not workspace.is_contiguous():   # (its bytes would not be numel of them, one after another)
-            raise ValueError("workspace: must be contiguous")
-        ws_bytes = workspace.numel() * workspace.element_size()
+        ws_bytes = _workspace_size(workspace, dev)
     elif n > 0 and paged_workspace_bytes(desc, n) > 0:
         workspace = _scratch_on(stream, lambda: alloc_paged_workspace(desc, n, q.device))
         ws_bytes = workspace.numel()
@@ -594,4 +620,226 @@ def pbb_paged_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, out
         _stream_on(stream, dev))
     if status != PBB_OK:
         raise PbbError("pbb_paged_attention", status)
+    return out
+
+
+# ------------------------------------------------------------------------------------------
+# Norms of queries and keys with the rotation
+
+def _norm_of(eps, q_weight, k_weight, d: int, dtype, dev: int) -> PbbNorm:
+    if q_weight is not None:
+        _dense("q_weight", q_weight, (d,), dtype, dev)
+    if k_weight is not None:
+        _dense("k_weight", k_weight, (d,), dtype, dev)
+    return PbbNorm(eps, _ptr(q_weight), _ptr(k_weight))
+
+
+def _norm_call(rope, positions, q, k):
+    """(device, dtype code, tokens, Hq, Hkv, d, positions' address) of a norm call."""
+    dev = _device_for("q", q, "[tokens][Hq][d]")
+    n, hq, d = q.shape
+    code = DTYPE_BF16 if q.dtype is torch.bfloat16 else DTYPE_F32 if q.dtype is torch.float32 else -1
+    hkv = 0
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+            raise ValueError("k: must be [tokens][Hkv][d]")
+        hkv = k.shape[1]
+    at = 0
+    if rope is not None:
+        one = rope.n_axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1
+        _dense("positions", positions, (n,) if one else (rope.n_axes, n), torch.int32, dev)
+        at = positions.data_ptr()
+    return dev, code, n, hq, hkv, d, at
+
+
+def pbb_norm_rotate(rope, positions, q, q_out, k=None, k_out=None, q_weight=None, k_weight=None,
+                    eps: float = 1e-6, stream=None):
+    """Rows ``q`` [tokens][Hq][d] (and ``k`` [tokens][Hkv][d]) divided by their root mean square, times
+    their weight [d] (None: ones), turned by ``positions`` as :func:`pbb_rotate` does (``rope`` None: not
+    turned), into ``q_out`` and ``k_out``, in one launch (see ``include/pbb.h``).  Tokens may lie apart; an
+    output may be its input."""
+    dev, code, n, hq, hkv, d, at = _norm_call(rope, positions, q, k)
+    dtype = q.dtype
+    if (k is None) != (k_out is None):
+        raise ValueError("pbb_norm_rotate: pass both k and k_out or neither")
+    qs, qos, ks, kos = _rows("q", q, (n, hq, d), dtype, dev), _rows("q_out", q_out, (n, hq, d), dtype, dev), 0, 0
+    if k is not None:
+        ks, kos = _rows("k", k, (n, hkv, d), dtype, dev), _rows("k_out", k_out, (n, hkv, d), dtype, dev)
+    status = load_library().pbb_norm_rotate(
+        _norm_of(eps, q_weight, k_weight, d, dtype, dev), rope, d, n, hq, hkv, at, q.data_ptr(), qs,
+        q_out.data_ptr(), qos, _ptr(k), ks, _ptr(k_out), kos, code, _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_norm_rotate", status)
+
+
+def norm_workspace_bytes(n_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype) -> int:
+    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}.get(dtype, dtype)
+    out = ctypes.c_size_t()
+    _check("pbb_norm_workspace_bytes", load_library().pbb_norm_workspace_bytes(
+        int(head_dim), int(n_tokens), int(n_q_heads), int(n_kv_heads), int(code), ctypes.byref(out)))
+    return out.value
+
+
+def alloc_norm_workspace(n_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype,
+                         device="cuda"):
+    """Workspace for :func:`pbb_norm_rotate_backward` calls of these sizes (contents irrelevant; calls that
+    may overlap need their own)."""
+    n = norm_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype)
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def pbb_norm_rotate_backward(rope, positions, q, q_grad, dq, k=None, k_grad=None, dk=None, q_weight=None,
+                             k_weight=None, dq_weight=None, dk_weight=None, eps: float = 1e-6,
+                             workspace=None, stream=None):
+    """Gradients of :func:`pbb_norm_rotate` (whose inputs ``q`` and ``k`` are) for the gradients ``q_grad``
+    and ``k_grad`` of its outputs: ``dq`` and ``dk``, and the weights' ``dq_weight`` and ``dk_weight``
+    (float32 [d], None: not wanted).  ``dq`` may be ``q_grad`` or ``q``.  Allocates the workspace when none
+    is given."""
+    dev, code, n, hq, hkv, d, at = _norm_call(rope, positions, q, k)
+    dtype = q.dtype
+    if (k is None) != (k_grad is None) or (k is None) != (dk is None):
+        raise ValueError("pbb_norm_rotate_backward: pass k, k_grad and dk, or none of them")
+    if k is None and dk_weight is not None:
+        raise ValueError("pbb_norm_rotate_backward: dk_weight without k")
+    shape = (n, hq, d)
+    qs, gs, dqs = (_rows(m, t, shape, dtype, dev) for m, t in (("q", q), ("q_grad", q_grad), ("dq", dq)))
+    ks = kgs = dks = 0
+    if k is not None:
+        shape = (n, hkv, d)
+        ks, kgs, dks = (_rows(m, t, shape, dtype, dev)
+                        for m, t in (("k", k), ("k_grad", k_grad), ("dk", dk)))
+    for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
+        if t is not None:
+            _dense(name, t, (d,), torch.float32, dev)
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = _workspace_size(workspace, dev)
+    elif n > 0 and (dq_weight is not None or dk_weight is not None):
+        workspace = _scratch_on(stream, lambda: alloc_norm_workspace(n, hq, hkv, d, dtype, q.device))
+        ws_bytes = workspace.numel()
+    status = load_library().pbb_norm_rotate_backward(
+        _norm_of(eps, q_weight, k_weight, d, dtype, dev), rope, d, n, hq, hkv, at, q.data_ptr(), qs,
+        q_grad.data_ptr(), gs, dq.data_ptr(), dqs, _ptr(k), ks, _ptr(k_grad), kgs, _ptr(dk), dks,
+        _ptr(dq_weight), _ptr(dk_weight), code, _ptr(workspace), ws_bytes, _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_norm_rotate_backward", status)
+
+
+# ------------------------------------------------------------------------------------------
+# 8-bit paged cache
+
+def scales_shape(desc: PbbPagedDesc):
+    return (desc.n_pages, desc.n_kv_heads, desc.page_size)
+
+
+def alloc_coded_pages(desc: PbbPagedDesc, device="cuda"):
+    """Allocate (uninitialised) K and V pages of e4m3 codes and their rows' scale bytes for ``desc``:
+    ``(k_pages, v_pages, k_scales, v_scales)``."""
+    pages = tuple(torch.empty(pages_shape(desc), dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
+    return pages + tuple(torch.empty(scales_shape(desc), dtype=torch.uint8, device=device) for _ in range(2))
+
+
+def coded_workspace_bytes(desc: PbbPagedDesc, n_tokens: int) -> int:
+    out = ctypes.c_size_t()
+    _check("pbb_coded_workspace_bytes", load_library().pbb_coded_workspace_bytes(
+        ctypes.byref(desc), int(n_tokens), ctypes.byref(out)))
+    return out.value
+
+
+def alloc_coded_workspace(desc: PbbPagedDesc, n_tokens: int, device="cuda"):
+    """Workspace for :func:`pbb_coded_attention` calls with ``desc``, by the rules of
+    :func:`alloc_paged_workspace`."""
+    return _counted_workspace(coded_workspace_bytes(desc, n_tokens), device)
+
+
+def _expect_coded(desc: PbbPagedDesc, pos, table, q_start, k_pages, v_pages, k_scales, v_scales, dev: int):
+    """The tensor checks that the 8-bit operators share; returns (Hq, Hkv, d)."""
+    batch, hkv, d = desc.batch, desc.n_kv_heads, desc.head_dim
+    if desc.dtype != DTYPE_BF16:
+        raise ValueError("desc: the 8-bit cache serves bfloat16 queries, keys and values")
+    _dense("pos", pos, (batch,), torch.int32, dev)
+    _dense("table", table, (batch, desc.table_width), torch.int32, dev)
+    if q_start is not None:
+        _dense("q_start", q_start, (batch + 1,), torch.int32, dev)
+    scales = (desc.n_pages, hkv, desc.page_size)
+    pages = scales + (d,)
+    _dense("k_pages", k_pages, pages, torch.float8_e4m3fn, dev)
+    _dense("v_pages", v_pages, pages, torch.float8_e4m3fn, dev)
+    _dense("k_scales", k_scales, scales, torch.uint8, dev)
+    _dense("v_scales", v_scales, scales, torch.uint8, dev)
+    return desc.n_q_heads, hkv, d
+
+
+def pbb_coded_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, k_scales, v_scales,
+                      q_start=None, rope=None, rope_pos=None, q=None, q_out=None, eps=None, q_weight=None,
+                      k_weight=None, stream=None):
+    """Append the new tokens of every sequence to an 8-bit cache (see ``include/pbb.h``): arguments as
+    :func:`pbb_paged_append`; with ``eps``, keys and queries are normalised and weighted as
+    :func:`pbb_norm_rotate` does before ``rope`` turns them."""
+    dev = _device_for("k", k, "[tokens][Hkv][d]")
+    n, dtype = k.shape[0], torch.bfloat16
+    hq, hkv, d = _expect_coded(desc, pos, table, q_start, k_pages, v_pages, k_scales, v_scales, dev)
+    kv = (n, hkv, d)
+    ks, vs, qs = _rows("k", k, kv, dtype, dev), _rows("v", v, kv, dtype, dev), 0
+    if (q is None) != (q_out is None):
+        raise ValueError("pbb_coded_append: pass both q and q_out or neither")
+    if q is not None:
+        qs = _rows("q", q, (n, hq, d), dtype, dev)
+        _dense("q_out", q_out, (n, hq, d), dtype, dev)
+    if rope_pos is not None:
+        if rope is None:
+            raise ValueError("pbb_coded_append: rope_pos without rope")
+        one = rope.n_axes == 1 and isinstance(rope_pos, torch.Tensor) and rope_pos.dim() == 1
+        _dense("rope_pos", rope_pos, (n,) if one else (rope.n_axes, n), torch.int32, dev)
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("pbb_coded_append: weights without eps")
+    norm = None if eps is None else _norm_of(eps, q_weight, k_weight, d, dtype, dev)
+    status = load_library().pbb_coded_append(
+        desc, n, pos.data_ptr(), _ptr(q_start), table.data_ptr(), norm, rope, _ptr(rope_pos), _ptr(q), qs,
+        _ptr(q_out), k.data_ptr(), ks, v.data_ptr(), vs, k_pages.data_ptr(), v_pages.data_ptr(),
+        k_scales.data_ptr(), v_scales.data_ptr(), _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_coded_append", status)
+
+
+def pbb_coded_read(desc: PbbPagedDesc, pos, table, k_pages, v_pages, k_scales, v_scales, k, v,
+                    q_start=None, stream=None):
+    """The values that the cache holds at the packed tokens' positions, into ``k`` and ``v``
+    [tokens][Hkv][d] (bfloat16, exact; see ``include/pbb.h``)."""
+    dev = _device_for("k", k, "[tokens][Hkv][d]")
+    n = k.shape[0]
+    _, hkv, d = _expect_coded(desc, pos, table, q_start, k_pages, v_pages, k_scales, v_scales, dev)
+    _dense("k", k, (n, hkv, d), torch.bfloat16, dev)
+    _dense("v", v, (n, hkv, d), torch.bfloat16, dev)
+    status = load_library().pbb_coded_read(
+        desc, n, pos.data_ptr(), _ptr(q_start), table.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+        k_scales.data_ptr(), v_scales.data_ptr(), k.data_ptr(), v.data_ptr(), _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_coded_read", status)
+    return k, v
+
+
+def pbb_coded_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, k_scales, v_scales, out,
+                         q_start=None, lse=None, workspace=None, stream=None):
+    """:func:`pbb_paged_attention` over an 8-bit cache (see ``include/pbb.h``).  ``workspace``: of
+    :func:`alloc_coded_workspace`, contiguous; allocated when none is given."""
+    dev = _device_for("q", q, "[tokens][Hq][d]")
+    n, dtype = q.shape[0], torch.bfloat16
+    hq, _, d = _expect_coded(desc, pos, table, q_start, k_pages, v_pages, k_scales, v_scales, dev)
+    qs = _rows("q", q, (n, hq, d), dtype, dev)
+    _dense("out", out, (n, hq, d), dtype, dev)
+    if lse is not None:
+        _dense("lse", lse, (hq, n), torch.float32, dev)
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = _workspace_size(workspace, dev)
+    elif n > 0 and coded_workspace_bytes(desc, n) > 0:
+        workspace = _scratch_on(stream, lambda: alloc_coded_workspace(desc, n, q.device))
+        ws_bytes = workspace.numel()
+    status = load_library().pbb_coded_attention(
+        desc, n, pos.data_ptr(), _ptr(q_start), table.data_ptr(), q.data_ptr(), qs, k_pages.data_ptr(),
+        v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), out.data_ptr(), _ptr(lse),
+        _ptr(workspace), ws_bytes, _stream_on(stream, dev))
+    if status != PBB_OK:
+        raise PbbError("pbb_coded_attention", status)
     return out
