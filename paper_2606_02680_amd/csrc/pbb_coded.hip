@@ -357,6 +357,16 @@ struct Wide {
   static constexpr int ALL = LDS > Narrow<D>::LDS ? LDS : Narrow<D>::LDS;
 };
 
+// read_chunks of 64 channels (those of the line that the addresses lie in).
+template <int D, int OFF>
+__device__ __forceinline__ void read_half_chunks(u32x2 (&dst)[8], const uint32_t (&ta)[4], uint32_t sb) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    dst[2 * x] = tr_read<OFF>(ta[x] + sb);
+    dst[2 * x + 1] = tr_read<OFF + 32 * D>(ta[x] + sb);
+  }
+}
+
 template <int D, int OCC>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(OCC)))
 void coded_kernel(CodedArgs a8) {
@@ -439,11 +449,14 @@ void coded_kernel(CodedArgs a8) {
   auto load = [&]() {   // the next step's rows: lane l takes a piece of row l / 8
     const bool ok0 = sh.is_page(id0), ok1 = sh.is_page(id1) && !past;
     gone |= (ok0 ? 0u : 1u) | (ok1 ? 0u : 2u);
-    const uint32_t id = wave >= 2 ? (ok1 ? (uint32_t)id1 : 0u) : (ok0 ? (uint32_t)id0 : 0u);
+    const bool second = wave >= 2;
+    const uint32_t id = (second ? ok1 : ok0) ? (uint32_t)(second ? id1 : id0) : 0u;
     const uint64_t row = ((uint64_t)id * (uint32_t)a.hkv + (uint32_t)g) * (uint32_t)sh.page_size + (uint32_t)slot;
+    // (offsets that the compiler takes as new: else it keeps four 64-bit addresses per lane)
+    uint32_t at = (uint32_t)lane * (4 * VW), r = (uint32_t)lane >> 3;
+    asm volatile("" : "+v"(at), "+v"(r));
     const unsigned char* const k = (const unsigned char*)a.k_pages + row * D;
     const unsigned char* const v = (const unsigned char*)a.v_pages + row * D;
-    const uint32_t at = (uint32_t)lane * (4 * VW);
     if constexpr (D == 128) {
       *(u32x4*)raw_k = *(const u32x4*)(k + at);
       *(u32x4*)raw_v = *(const u32x4*)(v + at);
@@ -451,8 +464,8 @@ void coded_kernel(CodedArgs a8) {
       *(u32x2*)raw_k = *(const u32x2*)(k + at);
       *(u32x2*)raw_v = *(const u32x2*)(v + at);
     }
-    raw_ks = (a8.k_scales + row)[lane >> 3];
-    raw_vs = (a8.v_scales + row)[lane >> 3];
+    raw_ks = (a8.k_scales + row)[r];
+    raw_vs = (a8.v_scales + row)[r];
     next_key += 32;
   };
   // where this lane's values go in a tile: row 8 wave + lane / 8, one piece of 8 values or two
@@ -495,13 +508,12 @@ void coded_kernel(CodedArgs a8) {
     const int cu = min(cp, tokens - 1);
     return Column{cu, col - cp * G, cp == cu};
   };
-  int tcol[QC], lo_c[QC];
+  int tcol[QC];
   bf16x8 qB[QC][KK];
 #pragma unroll
   for (int qc = 0; qc < QC; ++qc) {
     const Column x = column(qc, c16);
     tcol[qc] = x.valid ? t0 + x.cp : -1;
-    lo_c[qc] = sh.support_lo(t0 + x.cp);
     const unsigned char* qrow = (const unsigned char*)a.q + (row0 + x.cp) * a.q_stride +
                                 (int64_t)(g * G + x.head) * ROWB + 16 * j4;
 #pragma unroll
@@ -585,18 +597,16 @@ void coded_kernel(CodedArgs a8) {
     __builtin_amdgcn_sched_barrier(0);
     // Element e of s0 is key k0 + 4 j4 + e of the lane's column, of s1 key k0 + 16 + 4 j4 + e.
     const int k0 = (s_first + st) * 32 + 4 * j4;
-    auto seen = [&](int qc, int e) -> bool {   // element e: 0..3 of s0, 4..7 of s1
-      const int k = e < 4 ? e : e + 12;
-      return k >= lo_c[qc] - k0 && k <= tcol[qc] - k0 && !(dropped & (e < 4 ? 1u : 2u));
-    };
     if (masked) {
 #pragma unroll
-      for (int qc = 0; qc < QC; ++qc)
+      for (int qc = 0; qc < QC; ++qc) {
+        const int lo = sh.support_lo(tcol[qc]) - k0, hi = tcol[qc] - k0;   // (taken anew: registers)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s0[qc][e] = seen(qc, e) ? s0[qc][e] : kNegInf;
-          s1[qc][e] = seen(qc, 4 + e) ? s1[qc][e] : kNegInf;
+          s0[qc][e] = e >= lo && e <= hi && !(dropped & 1u) ? s0[qc][e] : kNegInf;
+          s1[qc][e] = e + 16 >= lo && e + 16 <= hi && !(dropped & 2u) ? s1[qc][e] : kNegInf;
         }
+      }
     }
     // The online softmax of the bf16 kernel, its weights rounded to bf16 for the value products, the sums
     // in 32 bits.
@@ -629,7 +639,6 @@ void coded_kernel(CodedArgs a8) {
 #pragma unroll
       for (int qc = 0; qc < QC; ++qc) m[qc] = fmaxf(m[qc], column_max(qc));
     }
-    u32x2 vr[2 * NB];
     if (__builtin_amdgcn_ballot_w64(weights()) != 0) {
 #pragma unroll
       for (int qc = 0; qc < QC; ++qc) {
@@ -645,23 +654,30 @@ void coded_kernel(CodedArgs a8) {
     }
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) lsum[qc] += ps[qc];
-    read_chunks<D, L::TILE>(vr, va, sb);
-    wait_chunks<D>(vr);
-    if (masked && __builtin_amdgcn_ballot_w64(any_special(vr)) != 0) {
-      odd = true;
+    // 64 channels' values at a time: 16 registers less than all at once, which the rows on their way need
+    auto values_of = [&](auto part) {
+      constexpr int H = decltype(part)::value;
+      u32x2 vr[8];
+      read_half_chunks<D, L::TILE + H * kTileLine>(vr, va, sb);
+      wait_chunks<64>(vr);
+      if (masked && __builtin_amdgcn_ballot_w64(any_special(vr)) != 0) {
+        odd = true;
 #pragma unroll
-      for (int i = 0; i < 2 * NB; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) vr[i][e] &= ~special_halves(vr[i][e]);
-    }
+          for (int e = 0; e < 2; ++e) vr[i][e] &= ~special_halves(vr[i][e]);
+      }
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const bf16x8 vt = join_chunks(vr[2 * nb], vr[2 * nb + 1]);
+      for (int i = 0; i < 4; ++i) {
+        const bf16x8 vt = join_chunks(vr[2 * i], vr[2 * i + 1]);
 #pragma unroll
-      for (int qc = 0; qc < QC; ++qc)
-        acc[qc][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pB[qc], acc[qc][nb], 0, 0, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+        for (int qc = 0; qc < QC; ++qc)
+          acc[qc][4 * H + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pB[qc], acc[qc][4 * H + i], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    values_of(std::integral_constant<int, 0>{});
+    if constexpr (D == 128) values_of(std::integral_constant<int, 1>{});
   };
 
   // (after next_rows(st), gone ends with the bits of step st + 2; before it, of step st + 1)
@@ -701,7 +717,7 @@ void coded_kernel(CodedArgs a8) {
             const float add = (x & 0x7F800000u) == 0x7F800000u ? __uint_as_float(x) : 0.0f;
 #pragma unroll
             for (int qc = 0; qc < QC; ++qc)
-              acc[qc][nb][e] += key >= lo_c[qc] && key <= tcol[qc] ? add : 0.0f;
+              acc[qc][nb][e] += key >= sh.support_lo(tcol[qc]) && key <= tcol[qc] ? add : 0.0f;
           }
         }
       }
@@ -713,7 +729,7 @@ void coded_kernel(CodedArgs a8) {
   for (int qc = 0; qc < QC; ++qc) {
     lsum[qc] = sum_xor16_32(lsum[qc]);
     if (__builtin_expect(lsum[qc] == 0.0f, 0) &&
-        any_page(sh, table, max(lo_c[qc], s_first * 32), min(tcol[qc], (s_first + nsteps) * 32 - 1)))
+        any_page(sh, table, max(sh.support_lo(tcol[qc]), s_first * 32), min(tcol[qc], (s_first + nsteps) * 32 - 1)))
       m[qc] = kNoWeight;
   }
   if (it.ways == 1) {
