@@ -377,7 +377,6 @@ void coded_kernel(CodedArgs a8) {
   constexpr int NB = D / 16;
   constexpr int ROWB = D * 2;           // bytes of a query or output row, and of a bf16 value row
   constexpr int KK = D / 32;            // 32-channel slices of the score contraction
-  constexpr int VW = D / 32;            // words of codes that a lane takes of 8 rows
   __shared__ __align__(1024) unsigned char smem[L::ALL];
 
   const int tid = threadIdx.x;
@@ -445,52 +444,49 @@ void coded_kernel(CodedArgs a8) {
     slot = next_key + 8 * wave - (wave >= 2 ? i1 : i0) * sh.page_size;
   };
   uint32_t gone = 0;
-  uint32_t raw_k[VW], raw_v[VW], raw_ks = 0, raw_vs = 0;
-  auto load = [&]() {   // the next step's rows: lane l takes a piece of row l / 8
+  u32x2 raw_k[D / 64], raw_v[D / 64];   // 8 codes of each line of the row
+  uint32_t raw_ks = 0, raw_vs = 0;
+  auto load = [&]() {   // the next step's rows: lane l takes 8 codes of each 64 of row l / 8
     const bool ok0 = sh.is_page(id0), ok1 = sh.is_page(id1) && !past;
     gone |= (ok0 ? 0u : 1u) | (ok1 ? 0u : 2u);
-    const bool second = wave >= 2;
-    const uint32_t id = (second ? ok1 : ok0) ? (uint32_t)(second ? id1 : id0) : 0u;
+    const uint32_t id0s = ok0 ? (uint32_t)id0 : 0u, id1s = ok1 ? (uint32_t)id1 : 0u;
+    const uint32_t id = wave >= 2 ? id1s : id0s;
     const uint64_t row = ((uint64_t)id * (uint32_t)a.hkv + (uint32_t)g) * (uint32_t)sh.page_size + (uint32_t)slot;
     // (offsets that the compiler takes as new: else it keeps four 64-bit addresses per lane)
-    uint32_t at = (uint32_t)lane * (4 * VW), r = (uint32_t)lane >> 3;
+    uint32_t r = (uint32_t)lane >> 3, at = D * r + 8 * ((uint32_t)lane & 7);
     asm volatile("" : "+v"(at), "+v"(r));
     const unsigned char* const k = (const unsigned char*)a.k_pages + row * D;
     const unsigned char* const v = (const unsigned char*)a.v_pages + row * D;
-    if constexpr (D == 128) {
-      *(u32x4*)raw_k = *(const u32x4*)(k + at);
-      *(u32x4*)raw_v = *(const u32x4*)(v + at);
-    } else {
-      *(u32x2*)raw_k = *(const u32x2*)(k + at);
-      *(u32x2*)raw_v = *(const u32x2*)(v + at);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      raw_k[i] = *(const u32x2*)(k + at + 64 * i);
+      raw_v[i] = *(const u32x2*)(v + at + 64 * i);
     }
     raw_ks = (a8.k_scales + row)[r];
     raw_vs = (a8.v_scales + row)[r];
     next_key += 32;
   };
-  // where this lane's values go in a tile: row 8 wave + lane / 8, one piece of 8 values or two
+  // where this lane's values go in a tile: row 8 wave + lane / 8, piece lane mod 8 of each line (so that 16
+  // lanes write 16 different pieces of a bank row)
   __attribute__((address_space(3))) unsigned char* lds0 = nullptr;
   uint32_t vw;
   {
-    const int r = 8 * wave + (lane >> 3), pc = lane & 7;
-    const uint32_t at = D == 128 ? (uint32_t)(tile_row<D>(r) + (pc >> 2) * kTileLine +
-                                              ((((2 * pc) & 7) ^ tile_swz(r)) << 4))
-                                 : (uint32_t)(tile_row<D>(r) + ((pc ^ tile_swz(r)) << 4));
-    vw = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + at;
+    const int r = 8 * wave + (lane >> 3);
+    vw = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem +
+         (uint32_t)(tile_row<D>(r) + (((lane & 7) ^ tile_swz(r)) << 4));
   }
   auto convert = [&](int stage) {
     const uint32_t to = vw + (uint32_t)(stage * L::STAGE);
-    const float ku = __uint_as_float(raw_ks << 23), vu = __uint_as_float(raw_vs << 23);
-    auto put = [&](uint32_t at, const uint32_t (&raw)[VW], float unit) {
+    auto put = [&](uint32_t at, const u32x2 (&raw)[D / 64], float unit) {
 #pragma unroll
-      for (int i = 0; i < VW / 2; ++i) {   // (the swizzle moves pairs of pieces: the second lies 16 bytes on)
-        const u32x4 x = {values2<false>(raw[2 * i], unit), values2<true>(raw[2 * i], unit),
-                         values2<false>(raw[2 * i + 1], unit), values2<true>(raw[2 * i + 1], unit)};
-        *(__attribute__((address_space(3))) u32x4*)(lds0 + at + 16 * i) = x;
+      for (int i = 0; i < D / 64; ++i) {
+        const u32x4 x = {values2<false>(raw[i][0], unit), values2<true>(raw[i][0], unit),
+                         values2<false>(raw[i][1], unit), values2<true>(raw[i][1], unit)};
+        *(__attribute__((address_space(3))) u32x4*)(lds0 + at + kTileLine * i) = x;
       }
     };
-    put(to, raw_k, ku);
-    put(to + L::TILE, raw_v, vu);
+    put(to, raw_k, __uint_as_float(raw_ks << 23));
+    put(to + L::TILE, raw_v, __uint_as_float(raw_vs << 23));
   };
 
   fetch();
