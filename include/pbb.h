@@ -444,7 +444,7 @@ pbb_status_t pbb_norm_rotate(const pbb_norm_t *norm, const pbb_rope_t *rope, int
  *              n_tokens == 0)
  * Deterministic.  workspace: pbb_norm_workspace_bytes bytes, 16-byte aligned, contents irrelevant; needed
  * with a weight's gradient only (PBB_ERR_WORKSPACE if NULL or smaller).  The size depends on the arguments
- * of its query alone and is at most 4104 * head_dim.
+ * of its query alone and is at most 16400 * head_dim.
  */
 pbb_status_t pbb_norm_workspace_bytes(int32_t head_dim, int32_t n_tokens, int32_t n_q_heads,
                                       int32_t n_kv_heads, int32_t dtype, size_t *bytes);

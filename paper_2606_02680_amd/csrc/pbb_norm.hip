@@ -31,6 +31,14 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
+// The sum over the 64 / PC lanes that hold the same piece of different rows, in all of them.
+template <int PC>
+__device__ __forceinline__ float piece_sum(float x) {
+  if constexpr (PC <= 4) x = add_dpp<0x124>(x);   // row_ror: 4 lanes on of sixteen
+  if constexpr (PC <= 8) x = add_dpp<0x128>(x);   // 8 lanes on
+  return sum_xor16_32(x);
+}
+
 // A piece of a weight, as floats (null: ones).
 template <typename T>
 struct Weights {
@@ -134,24 +142,32 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
   float dlo[N], dhi[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) dlo[e] = dhi[e] = 0.0f;
+  struct Pair { u32x4 xl, xh, gl, gh; };   // a row's piece and its gradient's
   for (int u = block; u < p.units; u += p.blocks) {
     const int64_t tok = ((int64_t)u * NW + wave) * p.tokens_per_wave + sub;
     if (tok >= a.n || sub >= p.tokens_per_wave) continue;
-    float cs[N], sn[N];
-    if (a.turn)
-      piece_turns<T>(a.rope, pc, [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; }, cs, sn);
     const unsigned char* x = (const unsigned char*)p.x + tok * p.x_stride + pc * 16;
     const unsigned char* gr = (const unsigned char*)p.grad + tok * p.grad_stride + pc * 16;
     unsigned char* o = (unsigned char*)p.out + tok * p.out_stride + pc * 16;
-    for (int h = row - sub * p.heads; h < p.heads; h += ROWS) {
+    auto load = [&](int h) -> Pair {
       const size_t at = (size_t)h * ROWB;
-      const u32x4 xl = load16<NT>(x + at), xh = load16<NT>(x + at + ROWB / 2);
-      const u32x4 gl = load16<NT>(gr + at), gh = load16<NT>(gr + at + ROWB / 2);
+      return Pair{load16<NT>(x + at), load16<NT>(x + at + ROWB / 2), load16<NT>(gr + at),
+                  load16<NT>(gr + at + ROWB / 2)};
+    };
+    // (the first rows' loads go out before the positions', whose sines and cosines are a chain of their own)
+    int h = row - sub * p.heads;
+    Pair r0 = load(min(h, p.heads - 1));
+    float cs[N], sn[N];
+    if (a.turn)
+      piece_turns<T>(a.rope, pc, [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; }, cs, sn);
+    for (; h < p.heads; h += ROWS) {
+      const size_t at = (size_t)h * ROWB;
+      const Pair v = r0;
       float f[N], g[N], y[N], z[N], ss = 0.0f, dot = 0.0f;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        f[e] = Piece<T>::get(xl, e), g[e] = Piece<T>::get(xh, e);
-        const float s = Piece<T>::get(gl, e), t = Piece<T>::get(gh, e);
+        f[e] = Piece<T>::get(v.xl, e), g[e] = Piece<T>::get(v.xh, e);
+        const float s = Piece<T>::get(v.gl, e), t = Piece<T>::get(v.gh, e);
         if (a.turn) rope_turn(s, t, cs[e], sn[e], y[e], z[e]);
         else y[e] = s, z[e] = t;
         ss = __builtin_fmaf(f[e], f[e], __builtin_fmaf(g[e], g[e], ss));
@@ -167,6 +183,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
         y[e] = r * __builtin_fmaf(-nl, s, y[e] * w.lo[e]);
         z[e] = r * __builtin_fmaf(-nh, s, z[e] * w.hi[e]);
       }
+      if (h + ROWS < p.heads) r0 = load(h + ROWS);
       store16<NT>(Piece<T>::put(y), o + at);
       store16<NT>(Piece<T>::put(z), o + at + ROWB / 2);
     }
@@ -174,11 +191,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
   if (p.dweight == nullptr) return;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-#pragma unroll
-    for (int x = PC; x < 64; x *= 2) {
-      dlo[e] += __shfl_xor(dlo[e], x);
-      dhi[e] += __shfl_xor(dhi[e], x);
-    }
+    dlo[e] = piece_sum<PC>(dlo[e]);
+    dhi[e] = piece_sum<PC>(dhi[e]);
     if (row == 0) {
       sums[wave][pc * N + e] = dlo[e];
       sums[wave][D / 2 + pc * N + e] = dhi[e];
@@ -196,10 +210,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
 }
 
 // Sums the workgroups' parts of the weights' gradients: 16 channels of a kind to a workgroup, whose
-// threads take every 16th part.
+// threads take every 64th part.
+constexpr int kSumThreads = 1024;
 template <int D>
-__global__ __launch_bounds__(kNormThreads) void norm_weight_sum_kernel(NormArgs a) {
-  constexpr int T = kNormThreads / 16;
+__global__ __launch_bounds__(kSumThreads) void norm_weight_sum_kernel(NormArgs a) {
+  constexpr int T = kSumThreads / 16;
   __shared__ float sums[T][16];
   const int kind = (int)blockIdx.x / (D / 16);
   const NormPart& p = a.part[kind];
@@ -212,10 +227,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_weight_sum_kernel(NormArgs 
   for (int i = t; i < p.blocks; i += T) s += parts[(size_t)i * D];
   sums[t][c] = s;
   __syncthreads();
-  if (t > 0) return;
+  if (threadIdx.x >= 64) return;   // the first wave: four threads a channel, then one
+  s = 0.0f;
 #pragma unroll
-  for (int i = 1; i < T; ++i) s += sums[i][c];
-  p.dweight[channel] = s;
+  for (int i = 0; i < T / 4; ++i) s += sums[4 * i + t][c];
+  s += __shfl_xor(s, 16);
+  s += __shfl_xor(s, 32);
+  if (t == 0) p.dweight[channel] = s;
 }
 
 template <typename T, int D>
@@ -267,7 +285,7 @@ hipError_t backward_t(const NormArgs& a0, hipStream_t stream) {
     p.tokens_per_wave = norm_tokens_per_wave(p.heads, ROWS);
     const int64_t per = (int64_t)WAVES * p.tokens_per_wave;
     p.units = (int32_t)((a.n + per - 1) / per);
-    p.blocks = norm_grad_blocks(a.n, p.heads, a.part[0].heads + a.part[1].heads, ROWS);
+    p.blocks = norm_grad_blocks(a.n, p.heads, a.part[0].heads + a.part[1].heads, ROWS, D * (int)sizeof(T));
     p.by_heads = FastDiv::make((uint32_t)p.heads);
     more |= p.dweight != nullptr && p.blocks != 1;
   }
@@ -280,7 +298,7 @@ hipError_t backward_t(const NormArgs& a0, hipStream_t stream) {
     hipLaunchKernelGGL((norm_rotate_backward_kernel<T, D, false>), grid, dim3(kNormThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !more) return e;
-  hipLaunchKernelGGL((norm_weight_sum_kernel<D>), dim3(2 * D / 16), dim3(kNormThreads), 0, stream, a);
+  hipLaunchKernelGGL((norm_weight_sum_kernel<D>), dim3(2 * D / 16), dim3(kSumThreads), 0, stream, a);
   return hipGetLastError();
 }
 

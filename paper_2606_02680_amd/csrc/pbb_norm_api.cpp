@@ -47,12 +47,11 @@ pbb::NormArgs norm_args(const pbb_norm_t* norm, const pbb_rope_t* rope, double s
   return a;
 }
 
-int rows_of_wave(int32_t head_dim, int32_t dtype) { return 64 / (int)(head_dim * elem_bytes(dtype) / 32); }
-
 size_t backward_bytes(int32_t head_dim, int32_t n, int32_t hq, int32_t hkv, int32_t dtype) {
-  const int rows = rows_of_wave(head_dim, dtype);
-  const int blocks = pbb::norm_grad_blocks(n, hq, hq + hkv, rows) + pbb::norm_grad_blocks(n, hkv, hq + hkv, rows);
-  return n > 0 ? (size_t)blocks * head_dim * sizeof(float) : 0;
+  const int row_bytes = (int)(head_dim * elem_bytes(dtype)), rows = 64 / (row_bytes / 32), all = hq + hkv;
+  const int blocks = pbb::norm_grad_blocks(n, hq, all, rows, row_bytes) +
+                     pbb::norm_grad_blocks(n, hkv, all, rows, row_bytes);
+  return (size_t)blocks * head_dim * sizeof(float);
 }
 
 }  // namespace
