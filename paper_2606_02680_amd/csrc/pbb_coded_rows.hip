@@ -6,8 +6,7 @@
 // of two is a bf16 value.
 //
 // Bound: HBM (each row read once and written once), small calls by the launch.  Append: a lane takes 8
-// channels and their partners d/2 further on, as in the rotation, and writes 8 codes of each half.  Read:
-// a lane takes 16 codes and writes 32 bytes.
+// channels and their partners d/2 further on, as in the rotation, and writes 8 codes of each half.
 
 #include "pbb_norm_internal.h"
 #include "pbb_coded_device.h"
@@ -101,9 +100,21 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
   const int sub = tpw > 1 ? a.by_rows.div(lane / PC) : 0;
   const int last = min((int)first + tpw - 1, a.n - 1);
   const int tok = min((int)first + sub, last);
+  const int pc = lane % PC;
+  const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
+  int r = blockIdx.y * a.run + lane / PC - sub * rows;
+  struct Pair { u32x4 lo, hi; };
+  auto load = [&](int i) -> Pair {   // (rows past the last: the last)
+    i = min(i, r1 - 1);
+    const unsigned char* src =
+        (i < hq ? (const unsigned char*)a.q + tok * a.q_stride + (size_t)i * ROWB
+         : i < hq + a.hkv ? (const unsigned char*)a.k + tok * a.k_stride + (size_t)(i - hq) * ROWB
+                          : (const unsigned char*)a.v + tok * a.v_stride + (size_t)(i - hq - a.hkv) * ROWB) + pc * 16;
+    return Pair{*(const u32x4*)src, *(const u32x4*)(src + ROWB / 2)};
+  };
+  Pair next = load(max(r, 0));   // (goes out before the search for the token's sequence and page)
   const Place at = place_of(a, tok, (int)first, last, lane);
   if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
-  const int pc = lane % PC;
   float cs[N], sn[N];
   if (a.turn)
     piece_turns<T>(a.rope, pc,
@@ -111,14 +122,10 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
                      return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : at.t;
                    },
                    cs, sn);
-  const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
-  for (int r = blockIdx.y * a.run + lane / PC - sub * rows; r < r1; r += ROWS) {
+  for (; r < r1; r += ROWS) {
     const bool query = r < hq, value = r >= hq + a.hkv;
-    const unsigned char* src =
-        (query ? (const unsigned char*)a.q + tok * a.q_stride + (size_t)r * ROWB
-         : !value ? (const unsigned char*)a.k + tok * a.k_stride + (size_t)(r - hq) * ROWB
-                  : (const unsigned char*)a.v + tok * a.v_stride + (size_t)(r - hq - a.hkv) * ROWB) + pc * 16;
-    const u32x4 lo = *(const u32x4*)src, hi = *(const u32x4*)(src + ROWB / 2);
+    const u32x4 lo = next.lo, hi = next.hi;
+    if (r + ROWS < r1) next = load(r + ROWS);
     float y[N], z[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = Piece<T>::get(lo, e), z[e] = Piece<T>::get(hi, e);
@@ -179,40 +186,62 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
   }
 }
 
-// Grid as the append's, over a token's key rows and value rows.
-template <int D>
+// Grid as the append's, over a token's key rows and value rows: 8 lanes to a row, each 8 codes of every 64,
+// so that a store's lanes write whole lines.
+constexpr int kReadRows = 8;
+template <int D, bool NT>
 __global__ __launch_bounds__(kRotThreads) void coded_read_kernel(CodedReadArgs a) {
-  constexpr int PC = D / 16;
-  constexpr int ROWS = 64 / PC;
   constexpr int ROWB = D * 2;
+  constexpr int P = D / 64;
+  constexpr int U = 2;   // rows of a lane in flight
   const int lane = threadIdx.x & 63;
   const int tpw = a.tokens_per_wave;
   const int64_t first = ((int64_t)token_group() * (kRotThreads / 64) +
                          __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * tpw;
   if (first >= a.n) return;
   const int rows = 2 * a.hkv;
-  const int sub = tpw > 1 ? a.by_rows.div(lane / PC) : 0;
+  const int sub = tpw > 1 ? a.by_rows.div(lane >> 3) : 0;
   const int last = min((int)first + tpw - 1, a.n - 1);
   const int tok = min((int)first + sub, last);
   const Place at = place_of(a, tok, (int)first, last, lane);
   if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
-  const int pc = lane % PC;
+  const int pc = lane & 7;
   const int r1 = min(rows, (int)(blockIdx.y + 1) * a.run);
-  for (int r = blockIdx.y * a.run + lane / PC - sub * rows; r < r1; r += ROWS) {
-    const bool value = r >= a.hkv;
-    const int h = r - (value ? a.hkv : 0);
-    u32x4 w = {0u, 0u, 0u, 0u};
-    float scale = 1.0f;
-    if (at.row >= 0) {
-      const int64_t row = at.row + (int64_t)h * a.shape.page_size;
-      w = *(const u32x4*)((value ? a.v_pages : a.k_pages) + row * D + pc * 16);
-      scale = power_of_two((int)(value ? a.v_scales : a.k_scales)[row] - 127);
-    }
-    unsigned char* o = (unsigned char*)(value ? a.v : a.k) + ((size_t)tok * a.hkv + h) * ROWB + pc * 32;
+  for (int r0 = blockIdx.y * a.run + (lane >> 3) - sub * rows; r0 < r1; r0 += U * kReadRows) {
+    u32x2 w[U][P];
+    uint32_t scale[U];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *(u32x4*)(o + 16 * i) = u32x4{values2<false>(w[2 * i], scale), values2<true>(w[2 * i], scale),
-                                    values2<false>(w[2 * i + 1], scale), values2<true>(w[2 * i + 1], scale)};
+    for (int u = 0; u < U; ++u) {
+      const int r = min(r0 + u * kReadRows, r1 - 1);
+      const bool value = r >= a.hkv;
+      const int64_t row = at.row + (int64_t)(r - (value ? a.hkv : 0)) * a.shape.page_size;
+      const uint8_t* const c = (value ? a.v_pages : a.k_pages) + row * D + pc * 8;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        w[u][i] = u32x2{0u, 0u};
+        if (at.row >= 0) {
+          if constexpr (NT) w[u][i] = __builtin_nontemporal_load((const u32x2*)(c + 64 * i));
+          else w[u][i] = *(const u32x2*)(c + 64 * i);
+        }
+      }
+      scale[u] = at.row >= 0 ? (value ? a.v_scales : a.k_scales)[row] : 127u;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * kReadRows;
+      if (r >= r1) break;
+      const bool value = r >= a.hkv;
+      const float unit = power_of_two((int)scale[u] - 127);
+      unsigned char* const o = (unsigned char*)(value ? a.v : a.k) +
+                               ((size_t)tok * a.hkv + (size_t)(r - (value ? a.hkv : 0))) * ROWB + pc * 16;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const u32x4 x = {values2<false>(w[u][i][0], unit), values2<true>(w[u][i][0], unit),
+                         values2<false>(w[u][i][1], unit), values2<true>(w[u][i][1], unit)};
+        if constexpr (NT) __builtin_nontemporal_store(x, (u32x4*)(o + 128 * i));
+        else *(u32x4*)(o + 128 * i) = x;
+      }
+    }
   }
 }
 
@@ -238,8 +267,11 @@ hipError_t append_t(const CodedAppendArgs& a0, hipStream_t stream) {
 template <int D>
 hipError_t read_t(const CodedReadArgs& a0, hipStream_t stream) {
   CodedReadArgs a = a0;
-  const dim3 grid = rows_grid(a, 2 * a.hkv, 64 / (D / 16));
-  hipLaunchKernelGGL((coded_read_kernel<D>), grid, dim3(kRotThreads), 0, stream, a);
+  const dim3 grid = rows_grid(a, 2 * a.hkv, kReadRows);
+  if ((int64_t)a.n * a.hkv * D * 4 > kStreamBytes)   // (of the rows written)
+    hipLaunchKernelGGL((coded_read_kernel<D, true>), grid, dim3(kRotThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((coded_read_kernel<D, false>), grid, dim3(kRotThreads), 0, stream, a);
   return hipGetLastError();
 }
 
