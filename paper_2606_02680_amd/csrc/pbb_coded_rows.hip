@@ -90,6 +90,7 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
   constexpr int ROWB = D * 2;
   constexpr int PC = ROWB / 32;
   constexpr int ROWS = 64 / PC;
+  __shared__ __align__(16) float2 turns[kRotThreads / 64][64];
   const int lane = threadIdx.x & 63;
   const int tpw = a.tokens_per_wave;
   const int64_t first = ((int64_t)token_group() * (kRotThreads / 64) +
@@ -112,16 +113,22 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
                           : (const unsigned char*)a.v + tok * a.v_stride + (size_t)(i - hq - a.hkv) * ROWB) + pc * 16;
     return Pair{*(const u32x4*)src, *(const u32x4*)(src + ROWB / 2)};
   };
-  Pair next = load(max(r, 0));   // (goes out before the search for the token's sequence and page)
+  // the first rows and the weights go out before the search for the token's sequence and page
+  Pair next = load(max(r, 0));
+  auto weight = [&](const void* w) -> Pair {
+    const unsigned char* p = (const unsigned char*)w + pc * 16;
+    const u32x4 one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    return w != nullptr ? Pair{*(const u32x4*)p, *(const u32x4*)(p + ROWB / 2)} : Pair{one, one};
+  };
+  const Pair wq = weight(a.q_weight), wk = weight(a.k_weight);
   const Place at = place_of(a, tok, (int)first, last, lane);
   if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
   float cs[N], sn[N];
-  if (a.turn)
-    piece_turns<T>(a.rope, pc,
-                   [&](int axis) {
-                     return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : at.t;
-                   },
-                   cs, sn);
+  if (a.turn) {
+    auto position = [&](int axis) { return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : at.t; };
+    if (tpw == 1) wave_turns<T, D>(a.rope, lane, pc, turns[threadIdx.x >> 6], position, cs, sn);
+    else piece_turns<T>(a.rope, pc, position, cs, sn);
+  }
   for (; r < r1; r += ROWS) {
     const bool query = r < hq, value = r >= hq + a.hkv;
     const u32x4 lo = next.lo, hi = next.hi;
@@ -130,21 +137,15 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = Piece<T>::get(lo, e), z[e] = Piece<T>::get(hi, e);
     if (a.norm && !value) {
-      const unsigned char* wp = (const unsigned char*)(query ? a.q_weight : a.k_weight);
       float ss = 0.0f;
 #pragma unroll
       for (int e = 0; e < N; ++e) ss = __builtin_fmaf(y[e], y[e], __builtin_fmaf(z[e], z[e], ss));
       const float rs = 1.0f / __builtin_sqrtf(__builtin_fmaf(row_sum<PC>(ss), 1.0f / D, a.eps));
-      if (wp != nullptr) {
-        const u32x4 wl = *(const u32x4*)(wp + pc * 16), wh = *(const u32x4*)(wp + ROWB / 2 + pc * 16);
+      const u32x4 wl = query ? wq.lo : wk.lo, wh = query ? wq.hi : wk.hi;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          y[e] = y[e] * rs * Piece<T>::get(wl, e);
-          z[e] = z[e] * rs * Piece<T>::get(wh, e);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] *= rs, z[e] *= rs;
+      for (int e = 0; e < N; ++e) {
+        y[e] = y[e] * rs * Piece<T>::get(wl, e);
+        z[e] = z[e] * rs * Piece<T>::get(wh, e);
       }
     }
     if (a.turn && !value) {

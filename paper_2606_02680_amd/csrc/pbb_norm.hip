@@ -68,6 +68,15 @@ __device__ __forceinline__ void store16(u32x4 v, unsigned char* p) {
   else *(u32x4*)p = v;
 }
 
+// The sines and cosines of this lane's piece of a row of token tok.
+template <typename T, int D>
+__device__ __forceinline__ void token_turns(const NormArgs& a, const NormPart& p, int64_t tok, int lane, int pc,
+                                            float2* turns, float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
+  auto position = [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; };
+  if (p.tokens_per_wave == 1) wave_turns<T, D>(a.rope, lane, pc, turns, position, cs, sn);
+  else piece_turns<T>(a.rope, pc, position, cs, sn);
+}
+
 // Workgroups 0 .. part[0].blocks - 1 take queries, the others keys.  A unit of work is a run of heads of
 // the tokens of a workgroup's waves; where a kind has fewer heads than a wave takes rows, a wave takes
 // several tokens.
@@ -77,6 +86,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_kernel(NormArgs a) {
   constexpr int ROWB = D * (int)sizeof(T);
   constexpr int PC = ROWB / 32;
   constexpr int ROWS = 64 / PC;
+  __shared__ __align__(16) float2 turns[kNormThreads / 64][64];
   const int lane = threadIdx.x & 63;
   const bool keys = (int)blockIdx.x >= a.part[0].blocks;
   const NormPart& p = a.part[keys ? 1 : 0];
@@ -91,8 +101,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_kernel(NormArgs a) {
     const int64_t tok = ((int64_t)group * (kNormThreads / 64) + (threadIdx.x >> 6)) * p.tokens_per_wave + sub;
     if (tok >= a.n) continue;
     float cs[N], sn[N];
-    if (a.turn)
-      piece_turns<T>(a.rope, pc, [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; }, cs, sn);
+    if (a.turn) token_turns<T, D>(a, p, tok, lane, pc, turns[threadIdx.x >> 6], cs, sn);
     const unsigned char* x = (const unsigned char*)p.x + tok * p.x_stride + pc * 16;
     unsigned char* o = (unsigned char*)p.out + tok * p.out_stride + pc * 16;
     const int h1 = min(p.heads, first + p.run);
@@ -131,6 +140,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
   constexpr int ROWS = 64 / PC;
   constexpr int NW = kNormThreads / 64;
   __shared__ float sums[NW][D];
+  __shared__ __align__(16) float2 turns[NW][64];
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
   const bool keys = (int)blockIdx.x >= a.part[0].blocks;
@@ -158,8 +168,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
     int h = row - sub * p.heads;
     Pair r0 = load(min(h, p.heads - 1));
     float cs[N], sn[N];
-    if (a.turn)
-      piece_turns<T>(a.rope, pc, [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; }, cs, sn);
+    if (a.turn) token_turns<T, D>(a, p, tok, lane, pc, turns[threadIdx.x >> 6], cs, sn);
     for (; h < p.heads; h += ROWS) {
       const size_t at = (size_t)h * ROWB;
       const Pair v = r0;

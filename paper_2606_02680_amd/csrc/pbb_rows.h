@@ -73,6 +73,27 @@ __device__ __forceinline__ void piece_turns(const RopeArgs& r, int pc, F&& posit
   }
 }
 
+// The same for a wave whose lanes all work on one token: each lane works out one pair and takes its piece's
+// from the others through LDS (`turns`: 64 float2 of the wave's own).  piece_turns does the work of a
+// token once per row of the wave, which its fp64 steps and, in fp32, its sines dominate (9070 tokens
+// appended: 48.7 us so, 40.0 shared; 4 x 16384 tokens normalised 245 and 231).
+template <typename T, int D, typename F>
+__device__ __forceinline__ void wave_turns(const RopeArgs& r, int lane, int pc, float2* turns, F&& position,
+                                           float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
+  constexpr int N = Piece<T>::N;
+  const int c = lane & (D / 2 - 1);
+  float2 t;
+  cos_sin<T>((double)position(r.axis[c]) * r.turns[c], t.x, t.y);
+  turns[lane] = t;
+  __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses keep their order)
+#pragma unroll
+  for (int e = 0; e < N; e += 2) {
+    const f32x4 two = *(const f32x4*)(turns + pc * N + e);
+    cs[e] = two[0], sn[e] = two[1], cs[e + 1] = two[2], sn[e + 1] = two[3];
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <typename T>
 __device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&cs)[Piece<T>::N],
                                             const float (&sn)[Piece<T>::N]) {
