@@ -19,7 +19,7 @@ pbb_status_t check_coded(const pbb_paged_desc_t* d, int32_t n) {
 }
 
 auto kind_of(const pbb_paged_desc_t* d) {
-  return [d](bool narrow) { return pbb::coded_kind(narrow, d->head_dim); };
+  return [d](bool narrow) { return pbb::coded_kind(narrow, d->head_dim, (int64_t)d->batch * d->n_kv_heads); };
 }
 
 bool cache_given(const void* kp, const void* vp, const void* ks, const void* vs) { return kp && vp && ks && vs; }

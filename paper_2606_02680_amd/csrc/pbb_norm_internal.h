@@ -120,7 +120,18 @@ struct CodedArgs {
   const uint8_t* v_scales;
 };
 
-inline PagedKind coded_kind(bool narrow, int head_dim) { return paged_kind(false, narrow, head_dim); }
+// Kinds of attention kernels over it: those of the bf16 cache (paged_kind has the reasons), but for two
+// rules.  Few columns: a step takes half the bytes, so that walks are cut into longer pieces where there are
+// many (256 tokens of 8 KV heads over PBB supports of up to 2048: 138 us, 156 with 64 steps; 64 tokens of 2
+// KV heads over up to 30000: 53, 58 with 128).  Many columns: 1280 pieces (nine chunks of 100 to 3000 over up
+// to 20000, 16/2 heads: 1267 us, 1336 with 1024; four of 512: 180 and 188; two chunks and 128 tokens: 198 and
+// 203, 211 with 1536).
+inline PagedKind coded_kind(bool narrow, int head_dim, int64_t units) {
+  PagedKind k = paged_kind(false, narrow, head_dim);
+  if (narrow && units >= 1024) k.many_least = 96;   // sequences times KV heads
+  if (!narrow) k.pieces = 1280;
+  return k;
+}
 
 hipError_t launch_norm_rotate(const NormArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
 hipError_t launch_norm_rotate_backward(const NormArgs& a, int32_t head_dim, bool f32, hipStream_t stream);
