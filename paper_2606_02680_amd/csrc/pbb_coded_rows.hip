@@ -124,10 +124,10 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
   const Place at = place_of(a, tok, (int)first, last, lane);
   if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
   float cs[N], sn[N];
-  if (a.turn) {
+  if (a.turn) {   // (to fp32: the hardware's sines, good to 2^-20, move twice as many values over a code's border)
     auto position = [&](int axis) { return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : at.t; };
-    if (tpw == 1) wave_turns<T, D>(a.rope, lane, pc, turns[threadIdx.x >> 6], position, cs, sn);
-    else piece_turns<T>(a.rope, pc, position, cs, sn);
+    if (tpw == 1) wave_turns<T, float, D>(a.rope, lane, pc, turns[threadIdx.x >> 6], position, cs, sn);
+    else piece_turns<T, float>(a.rope, pc, position, cs, sn);
   }
   for (; r < r1; r += ROWS) {
     const bool query = r < hq, value = r >= hq + a.hkv;

@@ -68,13 +68,14 @@ __device__ __forceinline__ void store16(u32x4 v, unsigned char* p) {
   else *(u32x4*)p = v;
 }
 
-// The sines and cosines of this lane's piece of a row of token tok.
+// The sines and cosines of this lane's piece of a row of token tok, to fp32 in bf16 too, as in the 8-bit
+// append (pbb_coded_rows.hip), whose queries are these bit for bit.
 template <typename T, int D>
 __device__ __forceinline__ void token_turns(const NormArgs& a, const NormPart& p, int64_t tok, int lane, int pc,
                                             float2* turns, float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
   auto position = [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; };
-  if (p.tokens_per_wave == 1) wave_turns<T, D>(a.rope, lane, pc, turns, position, cs, sn);
-  else piece_turns<T>(a.rope, pc, position, cs, sn);
+  if (p.tokens_per_wave == 1) wave_turns<T, float, D>(a.rope, lane, pc, turns, position, cs, sn);
+  else piece_turns<T, float>(a.rope, pc, position, cs, sn);
 }
 
 // Workgroups 0 .. part[0].blocks - 1 take queries, the others keys.  A unit of work is a run of heads of

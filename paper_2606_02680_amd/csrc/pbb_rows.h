@@ -61,15 +61,15 @@ __device__ __forceinline__ void cos_sin(double turns, float& cs, float& sn) {
 }
 
 // The sines and cosines of piece pc of a row (pairs pc N .. + N - 1) at a token's positions;
-// position(axis) reads them.
-template <typename T, typename F>
+// position(axis) reads them.  A: those of cos_sin<A>.
+template <typename T, typename A = T, typename F>
 __device__ __forceinline__ void piece_turns(const RopeArgs& r, int pc, F&& position,
                                             float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
   constexpr int N = Piece<T>::N;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     const int c = pc * N + e;
-    cos_sin<T>((double)position(r.axis[c]) * r.turns[c], cs[e], sn[e]);
+    cos_sin<A>((double)position(r.axis[c]) * r.turns[c], cs[e], sn[e]);
   }
 }
 
@@ -77,13 +77,13 @@ __device__ __forceinline__ void piece_turns(const RopeArgs& r, int pc, F&& posit
 // from the others through LDS (`turns`: 64 float2 of the wave's own).  piece_turns does the work of a
 // token once per row of the wave, which its fp64 steps and, in fp32, its sines dominate (9070 tokens
 // appended: 48.7 us so, 40.0 shared; 4 x 16384 tokens normalised 245 and 231).
-template <typename T, int D, typename F>
+template <typename T, typename A, int D, typename F>
 __device__ __forceinline__ void wave_turns(const RopeArgs& r, int lane, int pc, float2* turns, F&& position,
                                            float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
   constexpr int N = Piece<T>::N;
   const int c = lane & (D / 2 - 1);
   float2 t;
-  cos_sin<T>((double)position(r.axis[c]) * r.turns[c], t.x, t.y);
+  cos_sin<A>((double)position(r.axis[c]) * r.turns[c], t.x, t.y);
   turns[lane] = t;
   __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses keep their order)
 #pragma unroll
