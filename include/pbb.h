@@ -443,8 +443,9 @@ pbb_status_t pbb_norm_rotate(const pbb_norm_t *norm, const pbb_rope_t *rope, int
  *   dq_weight, dk_weight     optional float32 [head_dim], 4-byte aligned, overwritten (zeros for
  *              n_tokens == 0)
  * Deterministic.  workspace: pbb_norm_workspace_bytes bytes, 16-byte aligned, contents irrelevant; needed
- * with a weight's gradient only (PBB_ERR_WORKSPACE if NULL or smaller).  The size depends on the arguments
- * of its query alone and is at most 16400 * head_dim.
+ * with a weight's gradient only (PBB_ERR_WORKSPACE if NULL or smaller); calls that may run concurrently need
+ * workspaces of their own.  The size depends on the arguments of its query alone and is at most
+ * 16400 * head_dim.
  */
 pbb_status_t pbb_norm_workspace_bytes(int32_t head_dim, int32_t n_tokens, int32_t n_q_heads,
                                       int32_t n_kv_heads, int32_t dtype, size_t *bytes);
@@ -472,7 +473,8 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t *norm, const pbb_rope_t *
  * What an append stores of a row: the least power 2^e, -100 <= e <= 119, under which the row's largest finite
  * magnitude is at most 448 (the largest code), and the codes of the quotients, nearest, ties to even, finite
  * ones cut to 448 (rows above 2^119 * 448) -- so each value to half a step, 2^-4 of itself, or 2^-10 of 2^e
- * where that is more.  Infinities and NaN are stored as NaN.  Other writers may use any byte from 1 to 254.
+ * where that is more.  Infinities and NaN are stored as NaN.  Other writers may use any byte from 27 to 246
+ * (those exponents).  Of two tokens of a call that share a row, the codes and the byte may be of either.
  *
  * pbb_coded_append: arguments as pbb_paged_append; norm (optional) divides and weights keys and queries
  * as pbb_norm_rotate does, before rope turns them, all in fp32 and rounded once: to codes (keys), to

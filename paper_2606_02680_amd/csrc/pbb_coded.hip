@@ -25,7 +25,6 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kGroups = 2;             // 16-column groups of a wave
 static_assert(kPagedCols == 16 * kGroups * kWaves && kPagedStep == 32, "tile");
-typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
 // ------------------------------------------------------------------------------------------
 // LDS tiles of codes: blocks of 8 rows (8 D bytes), in lines of 128 bytes that hold 8 pieces of 16 bytes:
@@ -53,22 +52,6 @@ __device__ __forceinline__ uint32_t code_source(int lane) {
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   const uint32_t m = (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
   return m * 0xFFu;
-}
-
-// Whether one of the bf16 values of an operand is infinite or NaN, and the halves of a word that are.
-template <int N>
-__device__ __forceinline__ bool any_special(const u32x2 (&v)[N]) {
-  u16x2 top = {0, 0};
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[i][e] & 0x7FFF7FFFu));
-  return top[0] >= 0x7F80 || top[1] >= 0x7F80;
-}
-__device__ __forceinline__ uint32_t special_halves(uint32_t w) {
-  return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
-         ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -767,15 +750,20 @@ void coded_kernel(CodedArgs a8) {
 }
 
 // Calls of at most 16 columns per sequence, and all that they need: the last piece of a cut walk to end
-// merges them.
+// merges them.  Workgroup i runs on compute die i mod 8, so an item's KV heads go to one die, one after the
+// other: the scale bytes of a short page under all its heads share lines, which each die that reads one
+// fetches by itself (192 tokens over up to 32768 in pages of 16: 1060 us, 1073 with a head to a die, where a
+// request in eleven was for scale bytes; 256 over up to 2000: 106 and 112).
+constexpr int kDies = 8;
 template <int D>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(3)))
 void coded_narrow_kernel(CodedArgs a8) {
   __shared__ __align__(1024) unsigned char smem[Narrow<D>::LDS];
   const PagedArgs& a = a8.p;
   const int lane = threadIdx.x & 63;
-  const int item = a.plan.by_hkv.div((int)blockIdx.x);
-  const int g = (int)blockIdx.x - item * a.hkv;
+  const int turn = (int)(blockIdx.x / kDies), eight = a.plan.by_hkv.div(turn);
+  const int item = eight * kDies + (int)(blockIdx.x % kDies);
+  const int g = turn - eight * a.hkv;
   PagedItem it;
   if (!find_item<false>(a, item, lane, it)) return;
   narrow_walk<D, true>(a8, it, g, smem);
@@ -785,7 +773,8 @@ template <int D, int OCC>
 hipError_t attention_t(const CodedArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)(a.p.plan.items() * a.p.hkv));
   if (a.p.plan.narrow) {
-    hipLaunchKernelGGL((coded_narrow_kernel<D>), grid, dim3(kWaves * 64), 0, stream, a);
+    const int64_t eights = (a.p.plan.items() + kDies - 1) / kDies;
+    hipLaunchKernelGGL((coded_narrow_kernel<D>), dim3((unsigned)(eights * kDies * a.p.hkv)), dim3(kWaves * 64), 0, stream, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((coded_kernel<D, OCC>), grid, dim3(kWaves * 64), 0, stream, a);

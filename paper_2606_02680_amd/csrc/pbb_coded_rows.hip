@@ -69,18 +69,6 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {   // over the PC (4 or
   if constexpr (PC >= 8) x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));
   return x;
 }
-template <int PC>
-__device__ __forceinline__ float row_sum(float x) {
-  auto from = [](float v, auto ctrl) {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v),
-                                                                 decltype(ctrl)::value, 0xf, 0xf, true));
-  };
-  x += from(x, std::integral_constant<int, 0xB1>{});
-  x += from(x, std::integral_constant<int, 0x4E>{});
-  if constexpr (PC >= 8) x += from(x, std::integral_constant<int, 0x141>{});
-  return x;
-}
-
 // Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's query rows, key rows and
 // value rows (in this order).
 template <int D>

@@ -16,21 +16,6 @@
 namespace pbb {
 namespace {
 
-// The sum over the PC (4, 8 or 16) adjacent lanes that hold a row, in all of them, bit for bit the same
-// in each (partners' sums are added pairwise).
-template <int CTRL>
-__device__ __forceinline__ float add_dpp(float x) {
-  return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
-}
-template <int PC>
-__device__ __forceinline__ float row_sum(float x) {
-  x = add_dpp<0xB1>(x);                        // quad_perm: lane ^ 1
-  x = add_dpp<0x4E>(x);                        // lane ^ 2
-  if constexpr (PC >= 8) x = add_dpp<0x141>(x);   // row_half_mirror: the other quad of eight
-  if constexpr (PC >= 16) x = add_dpp<0x140>(x);  // row_mirror: the other eight of sixteen
-  return x;
-}
-
 // The sum over the 64 / PC lanes that hold the same piece of different rows, in all of them.
 template <int PC>
 __device__ __forceinline__ float piece_sum(float x) {

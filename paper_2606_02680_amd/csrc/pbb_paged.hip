@@ -37,25 +37,6 @@ static_assert(kPagedCols == 16 * kPagedGroups * kPagedWaves && kPagedStep == 32,
 // LDS stages and waves per SIMD that the registers are budgeted for (see the prefill).
 constexpr int kPagedStages128 = 3, kPagedOcc128 = 3;
 constexpr int kPagedStages64 = 4, kPagedOcc64 = 4;
-typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
-
-// Whether one of the bf16 values of an operand is infinite or NaN.
-template <int N>
-__device__ __forceinline__ bool any_special(const u32x2 (&v)[N]) {
-  u16x2 top = {0, 0};
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[i][e] & 0x7FFF7FFFu));
-  return top[0] >= 0x7F80 || top[1] >= 0x7F80;
-}
-
-// The halves of a word of two bf16 values that are infinite or NaN.
-__device__ __forceinline__ uint32_t special_halves(uint32_t w) {
-  return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
-         ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-}
 
 // Few columns: tiles of at most 16 (single tokens, short drafts).  The 16-key halves of the piece's
 // steps are dealt to the waves one by one, each with LDS tiles of its own, so that nothing but the

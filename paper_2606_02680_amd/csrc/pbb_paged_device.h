@@ -29,6 +29,26 @@ __device__ __forceinline__ void wait_tile(u32x2 (&v)[D / 16]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
 }
 
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+
+// Whether one of the bf16 values of an operand is infinite or NaN.
+template <int N>
+__device__ __forceinline__ bool any_special(const u32x2 (&v)[N]) {
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[i][e] & 0x7FFF7FFFu));
+  return top[0] >= 0x7F80 || top[1] >= 0x7F80;
+}
+
+// The halves of a word of two bf16 values that are infinite or NaN.
+__device__ __forceinline__ uint32_t special_halves(uint32_t w) {
+  return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
+         ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+
 // Device-coherent store and load of two floats (8 bytes, aligned): agent-scope atomics, which on this
 // chip go through to and come from the point where its compute dies meet, past their own caches.  A
 // state published with these stores is complete for whoever reads it with these loads after a counter

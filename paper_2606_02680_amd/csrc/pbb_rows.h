@@ -106,6 +106,21 @@ __device__ __forceinline__ void turn_pieces(u32x4& lo, u32x4& hi, const float (&
   hi = Piece<T>::put(oy);
 }
 
+// The sum over the PC (4, 8 or 16) adjacent lanes that hold a row, in all of them, bit for bit the same
+// in each (partners' sums are added pairwise).
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float x) {
+  return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+template <int PC>
+__device__ __forceinline__ float row_sum(float x) {
+  x = add_dpp<0xB1>(x);                        // quad_perm: lane ^ 1
+  x = add_dpp<0x4E>(x);                        // lane ^ 2
+  if constexpr (PC >= 8) x = add_dpp<0x141>(x);   // row_half_mirror: the other quad of eight
+  if constexpr (PC >= 16) x = add_dpp<0x140>(x);  // row_mirror: the other eight of sixteen
+  return x;
+}
+
 // The sequence that packed row `tok` belongs to, or -1: the number of sequences whose rows end at or
 // before it (every lane of the wave takes part; q_start never falls).
 __device__ __forceinline__ int sequence_of(const int32_t* q_start, int batch, int tok, int lane) {

@@ -633,6 +633,26 @@ def test_no_tokens(cuda):
         assert (bits(t.view(U8).view(torch.int16)) == b).all()
 
 
+def test_more_threads_than_a_grid_row(cuda):
+    """2^27 and some tokens read: more threads than the first dimension of a grid holds.  All but the last
+    are of a skipped sequence, and become zeros."""
+    n, last, d = 1 << 27, 5, 64
+    desc = P.make_paged_desc(2, 1, 1, d, page_size=16, n_pages=1, table_width=1)
+    row = torch.randn(16, 1, d).to(BF)
+    codes, scales = C.encode(row)
+    pool = [codes.view(U8).view(1, 1, 16, d).to(cuda).view(torch.float8_e4m3fn)] * 2 + [scales.view(1, 1, 16).to(cuda)] * 2
+    pos = torch.tensor([-1, 3], dtype=torch.int32, device=cuda)
+    q_start = torch.tensor([0, n, n + last], dtype=torch.int32, device=cuda)
+    table = torch.zeros(2, 1, dtype=torch.int32, device=cuda)
+    k, v = (torch.full((n + last, 1, d), 5.0, dtype=BF, device=cuda) for _ in range(2))      # 17 GB each
+    P.pbb_coded_read(desc, pos, table, *pool, k, v, q_start=q_start)
+    want = C.values(codes, scales)[3:3 + last]
+    for t in (k, v):
+        assert torch.equal(t[-last:].cpu().double(), want) and not bool(t[:-last].any())
+    del k, v, t
+    torch.cuda.empty_cache()
+
+
 def test_binding_refusals(cuda):
     c = Coded([(20, 4)], 4, 2, 64, 16, seed=14)
     x = c.on(cuda)

@@ -132,6 +132,26 @@ def test_large(cuda, dtype, n, hq, hkv, d):
         assert bool(((s.double() - t).abs() <= 2 * C.U * 400 * size).all())
 
 
+def test_more_units_than_workgroups(cuda):
+    """2^28 and some tokens of one head, in place: workgroups take several units of work; the last tokens'
+    rows are those of a call of their own."""
+    n, last, d = 1 << 28, 70, 64
+    rope = P.make_rope(d, BASE)
+    x = torch.zeros(n + last, 1, d, dtype=BF, device=cuda)            # 34 GB
+    x[-last:] = torch.randn(last, 1, d, device=cuda).to(BF)
+    x[:last] = x[-last:]
+    pos = torch.arange(n + last, dtype=torch.int32, device=cuda)
+    ends = [(x[e].clone(), pos[e].clone()) for e in (slice(0, last), slice(n, n + last))]
+    P.pbb_norm_rotate(rope, pos, x, x)
+    for (rows, at), got in zip(ends, (x[:last], x[-last:])):
+        want = torch.empty_like(rows)
+        P.pbb_norm_rotate(rope, at, rows, want)
+        assert torch.equal(got, want)
+    assert not bool(x[last:n].any())
+    del x, pos, got
+    torch.cuda.empty_cache()
+
+
 def test_gradients_by_differences(cuda):
     """<dy, f(x + h e) - f(x - h e)> / 2h against dx and dw in fp32, at h where the truncation (h^2 times
     third derivatives, below 1 here) and the rounding (2^-22 of the sum of |dy y| over 2h) are small."""
