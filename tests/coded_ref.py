@@ -94,14 +94,14 @@ def backward_bound(x, grad, weight, eps, positions, axis, base, dtype, depth):
 def weight_depth(n, heads, all_heads, d, dtype):
     """Additions that a term of a weight's gradient goes through, at most: its lane's rows (units of work of
     four waves, as many to a workgroup as its share of 4096, or 64 KiB where 512 workgroups remain), the
-    wave's lanes, its workgroup's waves, and 64 threads' parts of the launch."""
+    wave's lanes, its workgroup's waves, 512 threads' parts of the launch, and those threads."""
     row_bytes = d * (2 if dtype == torch.bfloat16 else 4)
     rows = 64 // (row_bytes // 32)
     per = 4 * (rows // heads if heads < rows else 1)
     units = -(-n // per)
     share = max(1, 4096 * heads // all_heads)
     each = max(-(-units // share), min(-(-65536 // (3 * per * heads * row_bytes)), -(-units // 512)))
-    return each * -(-heads // rows) + 6 + 4 + -(-units // each // 64) + 1 + 18
+    return each * -(-heads // rows) + 6 + 4 + -(-(-(-units // each)) // 512) + 6 + 8
 
 
 # ------------------------------------------------------------------------------------------
