@@ -331,7 +331,16 @@ __device__ __forceinline__ void narrow_walk(const CodedArgs& a8, const PagedItem
 
 // ------------------------------------------------------------------------------------------
 // Many columns.  Each wave takes 8 of a step's key rows and 8 of its value rows into registers, two steps
-// ahead, and converts them into the bf16 tiles of the step after the one that it works on.
+// ahead, their scale bytes through the scalar cache, and converts them into the bf16 tiles of the step after
+// the one that it works on, under the score products of that one.  The rest of a step is the bf16 kernel's,
+// so both give the same bits from the same values.
+//
+// Bound: a step's matrix instructions (128 x 32 x D twice) and the softmax and conversions beside them, which
+// share the issue slots.  Five chunks of 300 to 2048 tokens over up to 30 thousand, 32/8 heads, D 128: 1412 us
+// (908 TFLOP/s; the bf16 cache's kernel, which moves its rows by DMA and converts nothing, 1359).  Measured
+// there: rows two steps ahead as DMA of codes into LDS stages and converted from there, which takes no
+// registers, 1568; a branch around the conversions of a last step, so that none run under the products, 1470;
+// scale bytes by vector loads and the table by 64-bit addresses, 1456.
 template <int D>
 struct Wide {
   static constexpr int TILE = 64 * D;               // 32 rows in bf16
@@ -348,6 +357,18 @@ __device__ __forceinline__ void read_half_chunks(u32x2 (&dst)[8], const uint32_t
     dst[2 * x] = tr_read<OFF>(ta[x] + sb);
     dst[2 * x + 1] = tr_read<OFF + 32 * D>(ta[x] + sb);
   }
+}
+
+// Table entry i >= 0, through the scalar cache, by a 32-bit byte offset (a width is at most 2^26; the 64-bit
+// sum costs scalar registers and instructions in every step).
+__device__ __forceinline__ int entry(const int32_t* table, int i) {
+  typedef const __attribute__((address_space(4))) char* Bytes;
+  return *(const __attribute__((address_space(4))) int32_t*)((Bytes)(const void*)table + (uint32_t)i * 4u);
+}
+
+// Eight bytes that the launch does not write, through the scalar cache.
+__device__ __forceinline__ uint64_t scalar_long(const uint8_t* p) {
+  return *(const __attribute__((address_space(4))) uint64_t*)(const void*)p;
 }
 
 template <int D, int OCC>
@@ -421,23 +442,25 @@ void coded_kernel(CodedArgs a8) {
   int slot = 0;                  // this wave's rows in their page
   auto fetch = [&]() {
     const int i0 = sh.by_page.div(next_key), i1 = sh.by_page.div(next_key + 16);
-    id0 = scalar_word(table, min(i0, sh.width - 1));
-    id1 = scalar_word(table, min(i1, sh.width - 1));
+    id0 = entry(table, min(i0, sh.width - 1));
+    id1 = entry(table, min(i1, sh.width - 1));
     past = i1 >= sh.width;
     slot = next_key + 8 * wave - (wave >= 2 ? i1 : i0) * sh.page_size;
   };
   uint32_t gone = 0;
+  const uint64_t page_rows = (uint64_t)(uint32_t)a.hkv * (uint32_t)sh.page_size;
+  const uint64_t head_row = (uint64_t)(uint32_t)g * (uint32_t)sh.page_size;
   u32x2 raw_k[D / 64], raw_v[D / 64];   // 8 codes of each line of the row
-  uint32_t raw_ks = 0, raw_vs = 0;
+  uint64_t raw_ks = 0, raw_vs = 0;      // the 8 rows' scale bytes, through the scalar cache
   auto load = [&]() {   // the next step's rows: lane l takes 8 codes of each 64 of row l / 8
     const bool ok0 = sh.is_page(id0), ok1 = sh.is_page(id1) && !past;
     gone |= (ok0 ? 0u : 1u) | (ok1 ? 0u : 2u);
     const uint32_t id0s = ok0 ? (uint32_t)id0 : 0u, id1s = ok1 ? (uint32_t)id1 : 0u;
     const uint32_t id = wave >= 2 ? id1s : id0s;
-    const uint64_t row = ((uint64_t)id * (uint32_t)a.hkv + (uint32_t)g) * (uint32_t)sh.page_size + (uint32_t)slot;
-    // (offsets that the compiler takes as new: else it keeps four 64-bit addresses per lane)
-    uint32_t r = (uint32_t)lane >> 3, at = D * r + 8 * ((uint32_t)lane & 7);
-    asm volatile("" : "+v"(at), "+v"(r));
+    const uint64_t row = (uint64_t)id * page_rows + head_row + (uint32_t)slot;
+    // (an offset that the compiler takes as new: else it keeps 64-bit addresses per lane)
+    uint32_t at = D * ((uint32_t)lane >> 3) + 8 * ((uint32_t)lane & 7);
+    asm volatile("" : "+v"(at));
     const unsigned char* const k = (const unsigned char*)a.k_pages + row * D;
     const unsigned char* const v = (const unsigned char*)a.v_pages + row * D;
 #pragma unroll
@@ -445,8 +468,8 @@ void coded_kernel(CodedArgs a8) {
       raw_k[i] = *(const u32x2*)(k + at + 64 * i);
       raw_v[i] = *(const u32x2*)(v + at + 64 * i);
     }
-    raw_ks = (a8.k_scales + row)[r];
-    raw_vs = (a8.v_scales + row)[r];
+    raw_ks = scalar_long(a8.k_scales + row);
+    raw_vs = scalar_long(a8.v_scales + row);
     next_key += 32;
   };
   // where this lane's values go in a tile: row 8 wave + lane / 8, piece lane mod 8 of each line (so that 16
@@ -468,8 +491,9 @@ void coded_kernel(CodedArgs a8) {
         *(__attribute__((address_space(3))) u32x4*)(lds0 + at + kTileLine * i) = x;
       }
     };
-    put(to, raw_k, __uint_as_float(raw_ks << 23));
-    put(to + L::TILE, raw_v, __uint_as_float(raw_vs << 23));
+    const uint32_t mine = (uint32_t)lane & 56u;   // this lane's row's byte of the 8
+    put(to, raw_k, __uint_as_float((uint32_t)(raw_ks >> mine) << 23 & 0x7F800000u));
+    put(to + L::TILE, raw_v, __uint_as_float((uint32_t)(raw_vs >> mine) << 23 & 0x7F800000u));
   };
 
   fetch();
@@ -545,9 +569,8 @@ void coded_kernel(CodedArgs a8) {
     lds_barrier();
     return (uint32_t)((st & 1) * L::STAGE);
   };
-  // The rows of step st + 1 into their tiles, and the loads of step st + 2's.
+  // The loads of step st + 2's rows.
   auto next_rows = [&](int st) {
-    if (st + 1 < nsteps) convert((st + 1) & 1);
     gone <<= 2;
     if (st + 2 < nsteps) load();
     fetch();
@@ -571,6 +594,9 @@ void coded_kernel(CodedArgs a8) {
         s1[qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qB[qc][kk], s1[qc], 0, 0, 0);
       }
     }
+    // (step st + 1's rows, always: those of a step past the last go where nothing reads them, and without a
+    // branch the conversions run under the products)
+    convert((st + 1) & 1);
     __builtin_amdgcn_sched_barrier(0);
     next_rows(st);
     __builtin_amdgcn_sched_barrier(0);
@@ -661,13 +687,13 @@ void coded_kernel(CodedArgs a8) {
 
   // (after next_rows(st), gone ends with the bits of step st + 2; before it, of step st + 1)
   int st = 0;
-  for (; st < wlo && st < nsteps; ++st) begin_step(st), next_rows(st);
+  for (; st < wlo && st < nsteps; ++st) begin_step(st), convert((st + 1) & 1), next_rows(st);
   for (; st <= whi; ++st) {
     const uint32_t sb = begin_step(st);
     const uint32_t dropped = (gone >> 2) & 3u;
     step(st, sb, dropped, st < ua || st >= ub || dropped != 0);
   }
-  for (; st < nsteps; ++st) begin_step(st), next_rows(st);
+  for (; st < nsteps; ++st) begin_step(st), convert((st + 1) & 1), next_rows(st);
 
   if (odd) {
     // The infinities and NaN of masked steps, straight from the pages: their weights are positive,
