@@ -26,6 +26,15 @@ constexpr int kWaves = 4;
 constexpr int kGroups = 2;             // 16-column groups of a wave
 static_assert(kPagedCols == 16 * kGroups * kWaves && kPagedStep == 32, "tile");
 
+// Wave priorities: where several waves of a SIMD could issue, those in their products go first (their chain of
+// matrix instructions is what a step waits for), value products before score products, whose conversions run
+// along.  Five chunks 1407 -> 1360 us, four of 2000 to 4000 under a window of 4096 765 -> 735, D 64 287 ->
+// 272.  Few-column walks in such a launch go with score products, but for the issue of their loads: above all
+// but value products throughout, 130 sequences with two chunks took 184 us instead of 198, but 140 with
+// twelve short chunks, whose long walks then starve, 427 instead of 400; below them all the time, 64-channel
+// mixtures 158 instead of 146.  (300 with six chunks, D 64: 157, 151 without priorities.)
+constexpr int kNoPriority = 0, kScorePriority = 1, kValuePriority = 2;
+
 // ------------------------------------------------------------------------------------------
 // LDS tiles of codes: blocks of 8 rows (8 D bytes), in lines of 128 bytes that hold 8 pieces of 16 bytes:
 // at D = 128 line r is row r, at D = 64 line r holds rows r and r + 4.  A piece lies in slot
@@ -196,12 +205,14 @@ __device__ __forceinline__ void narrow_walk(const CodedArgs& a8, const PagedItem
   int stage = 0;
   for (; h < h1; h += NW) {
     // the half S - 1 ahead goes over the stage that the last half has left
+    if constexpr (!IN_PLACE) __builtin_amdgcn_s_setprio(kNoPriority);
     gone <<= 1;
     if (h + (S - 1) * NW < h1) issue(after, stage == 0 ? S - 1 : stage - 1);
     after = fetch(min(h + S * NW, h1 - 1));
     __builtin_amdgcn_sched_barrier(0);
     wait_groups<S - 1, L::OPS>(min(S - 1, (h1 - 1 - h) / NW));
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!IN_PLACE) __builtin_amdgcn_s_setprio(kScorePriority);
     const uint32_t sb = (uint32_t)(stage * L::STAGE);
     stage = stage == S - 1 ? 0 : stage + 1;
     const bool none = (gone >> (S - 1)) & 1u;
@@ -336,9 +347,9 @@ __device__ __forceinline__ void narrow_walk(const CodedArgs& a8, const PagedItem
 // so both give the same bits from the same values.
 //
 // Bound: a step's matrix instructions (128 x 32 x D twice) and the softmax and conversions beside them, which
-// share the issue slots.  Five chunks of 300 to 2048 tokens over up to 30 thousand, 32/8 heads, D 128: 1412 us
-// (908 TFLOP/s; the bf16 cache's kernel, which moves its rows by DMA and converts nothing, 1359).  Measured
-// there: rows two steps ahead as DMA of codes into LDS stages and converted from there, which takes no
+// share the issue slots.  Five chunks of 300 to 2048 tokens over up to 30 thousand, 32/8 heads, D 128: 1360 us
+// (943 TFLOP/s; the bf16 cache's kernel, which moves its rows by DMA and converts nothing, 1321).  Measured
+// there, without the priorities (1412): rows two steps ahead as DMA of codes into LDS stages and converted from there, which takes no
 // registers, 1568; a branch around the conversions of a last step, so that none run under the products, 1470;
 // scale bytes by vector loads and the table by 64-bit addresses, 1456.
 template <int D>
@@ -583,6 +594,7 @@ void coded_kernel(CodedArgs a8) {
       s0[qc] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       s1[qc] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+    __builtin_amdgcn_s_setprio(kScorePriority);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       const auto* kp = lds0 + ra[kk & 1] + sb + kTileLine * (kk >> 1);
@@ -598,6 +610,7 @@ void coded_kernel(CodedArgs a8) {
     // branch the conversions run under the products)
     convert((st + 1) & 1);
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(kNoPriority);
     next_rows(st);
     __builtin_amdgcn_sched_barrier(0);
     // Element e of s0 is key k0 + 4 j4 + e of the lane's column, of s1 key k0 + 16 + 4 j4 + e.
@@ -659,6 +672,7 @@ void coded_kernel(CodedArgs a8) {
     }
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) lsum[qc] += ps[qc];
+    __builtin_amdgcn_s_setprio(kValuePriority);
     // 64 channels' values at a time: 16 registers less than all at once, which the rows on their way need
     auto values_of = [&](auto part) {
       constexpr int H = decltype(part)::value;
@@ -683,6 +697,7 @@ void coded_kernel(CodedArgs a8) {
     };
     values_of(std::integral_constant<int, 0>{});
     if constexpr (D == 128) values_of(std::integral_constant<int, 1>{});
+    __builtin_amdgcn_s_setprio(kNoPriority);
   };
 
   // (after next_rows(st), gone ends with the bits of step st + 2; before it, of step st + 1)
