@@ -441,7 +441,8 @@ pbb_status_t pbb_norm_rotate(const pbb_norm_t *norm, const pbb_rope_t *rope, int
  *   q_grad, dq, k_grad, dk   rows as q and k, with strides of their own; dq may be q_grad or q, dk k_grad
  *              or k (same stride)
  *   dq_weight, dk_weight     optional float32 [head_dim], 4-byte aligned, overwritten (zeros for
- *              n_tokens == 0)
+ *              n_tokens == 0), two arrays (PBB_ERR_SHAPE where they overlap): a weight that queries and
+ *              keys share has the sum of both for its gradient
  * Deterministic.  workspace: pbb_norm_workspace_bytes bytes, 16-byte aligned, contents irrelevant; needed
  * with a weight's gradient only (PBB_ERR_WORKSPACE if NULL or smaller); calls that may run concurrently need
  * workspaces of their own.  The size depends on the arguments of its query alone and is at most
@@ -481,11 +482,11 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t *norm, const pbb_rope_t *
  * bfloat16 (q_out).  Values are quantised as they come.
  */
 pbb_status_t pbb_coded_append(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
-                               const int32_t *q_start, const int32_t *table, const pbb_norm_t *norm,
-                               const pbb_rope_t *rope, const int32_t *rope_pos, const void *q,
-                               int64_t q_stride, void *q_out, const void *k, int64_t k_stride,
-                               const void *v, int64_t v_stride, void *k_pages, void *v_pages,
-                               uint8_t *k_scales, uint8_t *v_scales, void *stream);
+                              const int32_t *q_start, const int32_t *table, const pbb_norm_t *norm,
+                              const pbb_rope_t *rope, const int32_t *rope_pos, const void *q,
+                              int64_t q_stride, void *q_out, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, void *k_pages, void *v_pages,
+                              uint8_t *k_scales, uint8_t *v_scales, void *stream);
 
 /*
  * Read cached rows back: k, v [n_tokens][n_kv_heads][head_dim] (bfloat16, contiguous) receive the values
@@ -495,25 +496,24 @@ pbb_status_t pbb_coded_append(const pbb_paged_desc_t *desc, int32_t n_tokens, co
  * left as they are.
  */
 pbb_status_t pbb_coded_read(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
-                             const int32_t *q_start, const int32_t *table, const void *k_pages,
-                             const void *v_pages, const uint8_t *k_scales, const uint8_t *v_scales,
-                             void *k, void *v, void *stream);
+                            const int32_t *q_start, const int32_t *table, const void *k_pages,
+                            const void *v_pages, const uint8_t *k_scales, const uint8_t *v_scales,
+                            void *k, void *v, void *stream);
 
 /*
  * Attention of the packed tokens over the 8-bit cache: pbb_paged_attention of the values that codes and
  * scales stand for, with its supports, masks, empty supports and log-partitions.  Scores are products of the
- * unquantised queries (rows of q down to 2^-22 of their largest magnitude) with fp32 accumulation; the
- * value products take weights as pbb_paged_attention does.  workspace: pbb_coded_workspace_bytes bytes,
- * by the rules of pbb_paged_workspace_bytes (its first PBB_PAGED_COUNTER_BYTES zero before the first call, and
- * left zero).
+ * unquantised queries with fp32 accumulation; the value products take weights as pbb_paged_attention does.
+ * workspace: pbb_coded_workspace_bytes bytes, by the rules of pbb_paged_workspace_bytes (its first
+ * PBB_PAGED_COUNTER_BYTES zero before the first call, and left zero).
  */
 pbb_status_t pbb_coded_workspace_bytes(const pbb_paged_desc_t *desc, int32_t n_tokens, size_t *bytes);
 
 pbb_status_t pbb_coded_attention(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
-                                  const int32_t *q_start, const int32_t *table, const void *q,
-                                  int64_t q_stride, const void *k_pages, const void *v_pages,
-                                  const uint8_t *k_scales, const uint8_t *v_scales, void *out, float *lse,
-                                  void *workspace, size_t workspace_bytes, void *stream);
+                                 const int32_t *q_start, const int32_t *table, const void *q,
+                                 int64_t q_stride, const void *k_pages, const void *v_pages,
+                                 const uint8_t *k_scales, const uint8_t *v_scales, void *out, float *lse,
+                                 void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

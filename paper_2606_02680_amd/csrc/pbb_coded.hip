@@ -66,7 +66,9 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 // ------------------------------------------------------------------------------------------
 // Few columns: tiles of at most 16 (single tokens, short drafts).  The 16-key halves of the piece's steps
 // are dealt to the waves one by one, each with LDS stages of its own (keys, values, scale bytes of a
-// half), so that nothing but the merge of the waves at the end waits for another wave.
+// half), so that nothing but the merge of the waves at the end waits for another wave.  Bound: HBM.  192
+// tokens over 256 to 32768, 32/8 heads, D 128 (6.75 GB): 1055 to 1065 us, 6.4 TB/s, where streaming reads reach
+// 6.5 (of the bf16 cache's twice the bytes: 2008 us); two or four stages, or four waves per SIMD: the same.
 template <int D>
 struct Narrow {
   static constexpr int STAGES = D == 128 ? 3 : 4;
@@ -318,7 +320,8 @@ __device__ __forceinline__ void narrow_walk(const CodedArgs& a8, const PagedItem
           const u32x2 c = *(const u32x2*)(row + 32 * nc);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (sees && (nan_bytes(c[i >> 2]) >> (8 * (i & 3)) & 1u)) acc[2 * nc + (i & 1)][i >> 1] = __builtin_nanf("");
+            if (sees && (nan_bytes(c[i >> 2]) >> (8 * (i & 3)) & 1u))
+              acc[2 * nc + (i & 1)][i >> 1] = __builtin_nanf("");
         }
       }
     }
@@ -346,12 +349,14 @@ __device__ __forceinline__ void narrow_walk(const CodedArgs& a8, const PagedItem
 // the one that it works on, under the score products of that one.  The rest of a step is the bf16 kernel's,
 // so both give the same bits from the same values.
 //
-// Bound: a step's matrix instructions (128 x 32 x D twice) and the softmax and conversions beside them, which
-// share the issue slots.  Five chunks of 300 to 2048 tokens over up to 30 thousand, 32/8 heads, D 128: 1360 us
-// (943 TFLOP/s; the bf16 cache's kernel, which moves its rows by DMA and converts nothing, 1321).  Measured
-// there, without the priorities (1412): rows two steps ahead as DMA of codes into LDS stages and converted from there, which takes no
-// registers, 1568; a branch around the conversions of a last step, so that none run under the products, 1470;
-// scale bytes by vector loads and the table by 64-bit addresses, 1456.
+// Bound: a step's matrix instructions (128 x 32 x D twice, a SIMD's matrix core 0.39 busy) and the softmax and
+// conversions beside them (its vector ALUs 0.6: an exponential takes four times as long as other
+// instructions), with the barrier's and the chain's waits between.  Five chunks of 300 to 2048 tokens over up
+// to 30 thousand, 32/8 heads, D 128: 1360 us (943 TFLOP/s; the bf16 cache's kernel, which moves its rows by
+// DMA and converts nothing, 1321).  Measured there, without the priorities (1412): rows two steps ahead as DMA
+// of codes into LDS stages and converted from there, which takes no registers, 1568; a branch around the
+// conversions of a last step, so that none run under the products, 1470; scale bytes by vector loads and the
+// table by 64-bit addresses, 1456.
 template <int D>
 struct Wide {
   static constexpr int TILE = 64 * D;               // 32 rows in bf16
@@ -815,7 +820,8 @@ hipError_t attention_t(const CodedArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)(a.p.plan.items() * a.p.hkv));
   if (a.p.plan.narrow) {
     const int64_t eights = (a.p.plan.items() + kDies - 1) / kDies;
-    hipLaunchKernelGGL((coded_narrow_kernel<D>), dim3((unsigned)(eights * kDies * a.p.hkv)), dim3(kWaves * 64), 0, stream, a);
+    hipLaunchKernelGGL((coded_narrow_kernel<D>), dim3((unsigned)(eights * kDies * a.p.hkv)), dim3(kWaves * 64), 0,
+                       stream, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((coded_kernel<D, OCC>), grid, dim3(kWaves * 64), 0, stream, a);

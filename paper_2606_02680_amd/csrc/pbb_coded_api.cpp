@@ -32,11 +32,11 @@ bool cache_aligned(const void* kp, const void* vp, const void* ks, const void* v
 extern "C" {
 
 pbb_status_t pbb_coded_append(const pbb_paged_desc_t* desc, int32_t n_tokens, const int32_t* pos,
-                               const int32_t* q_start, const int32_t* table, const pbb_norm_t* norm,
-                               const pbb_rope_t* rope, const int32_t* rope_pos, const void* q,
-                               int64_t q_stride, void* q_out, const void* k, int64_t k_stride,
-                               const void* v, int64_t v_stride, void* k_pages, void* v_pages,
-                               uint8_t* k_scales, uint8_t* v_scales, void* stream) {
+                              const int32_t* q_start, const int32_t* table, const pbb_norm_t* norm,
+                              const pbb_rope_t* rope, const int32_t* rope_pos, const void* q,
+                              int64_t q_stride, void* q_out, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, void* k_pages, void* v_pages,
+                              uint8_t* k_scales, uint8_t* v_scales, void* stream) {
   const pbb_status_t st = check_coded(desc, n_tokens);
   if (st != PBB_OK) return st;
   if (q_start == nullptr && n_tokens % desc->batch != 0) return PBB_ERR_SHAPE;
@@ -94,9 +94,9 @@ pbb_status_t pbb_coded_append(const pbb_paged_desc_t* desc, int32_t n_tokens, co
 }
 
 pbb_status_t pbb_coded_read(const pbb_paged_desc_t* desc, int32_t n_tokens, const int32_t* pos,
-                             const int32_t* q_start, const int32_t* table, const void* k_pages,
-                             const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales, void* k,
-                             void* v, void* stream) {
+                            const int32_t* q_start, const int32_t* table, const void* k_pages,
+                            const void* v_pages, const uint8_t* k_scales, const uint8_t* v_scales, void* k,
+                            void* v, void* stream) {
   const pbb_status_t st = check_coded(desc, n_tokens);
   if (st != PBB_OK) return st;
   if (q_start == nullptr && n_tokens % desc->batch != 0) return PBB_ERR_SHAPE;
@@ -134,10 +134,10 @@ pbb_status_t pbb_coded_workspace_bytes(const pbb_paged_desc_t* desc, int32_t n_t
 }
 
 pbb_status_t pbb_coded_attention(const pbb_paged_desc_t* desc, int32_t n_tokens, const int32_t* pos,
-                                  const int32_t* q_start, const int32_t* table, const void* q,
-                                  int64_t q_stride, const void* k_pages, const void* v_pages,
-                                  const uint8_t* k_scales, const uint8_t* v_scales, void* out, float* lse,
-                                  void* workspace, size_t workspace_bytes, void* stream) {
+                                 const int32_t* q_start, const int32_t* table, const void* q,
+                                 int64_t q_stride, const void* k_pages, const void* v_pages,
+                                 const uint8_t* k_scales, const uint8_t* v_scales, void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
   const pbb_status_t st = check_coded(desc, n_tokens);
   if (st != PBB_OK) return st;
   if (q_start == nullptr && n_tokens % desc->batch != 0) return PBB_ERR_SHAPE;

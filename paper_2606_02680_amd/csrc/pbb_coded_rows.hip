@@ -6,7 +6,9 @@
 // of two is a bf16 value.
 //
 // Bound: HBM (each row read once and written once), small calls by the launch.  Append: a lane takes 8
-// channels and their partners d/2 further on, as in the rotation, and writes 8 codes of each half.
+// channels and their partners d/2 further on, as in the rotation, and writes 8 codes of each half.  9070
+// tokens of 32/8 heads, d 128, normed and turned: 40.2 us, 5.1 TB/s with its inputs in the last-level cache
+// (48.7 with the sines of a token worked out by each of its rows' lanes); 256 tokens: 5.5 us.
 
 #include "pbb_norm_internal.h"
 #include "pbb_coded_device.h"
@@ -176,7 +178,8 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
 }
 
 // Grid as the append's, over a token's key rows and value rows: 8 lanes to a row, each 8 codes of every 64,
-// so that a store's lanes write whole lines.
+// so that a store's lanes write whole lines.  Six sequences of up to 32768 tokens, 8 heads, d 128 (748 MB): 140
+// us, 5.3 TB/s; the 9070 tokens above 12.3 us.
 constexpr int kReadRows = 8;
 template <int D, bool NT>
 __global__ __launch_bounds__(kRotThreads) void coded_read_kernel(CodedReadArgs a) {

@@ -32,6 +32,12 @@ pbb_status_t check_norm(const pbb_norm_t* norm, const pbb_rope_t* rope, int32_t 
 // Rows that a call reads and writes in place share their strides.
 bool in_place_ok(const void* x, int64_t xs, const void* out, int64_t os) { return out != x || os == xs; }
 
+// Two sums of head_dim floats, where both are wanted, are written by different workgroups.
+bool sums_apart(const float* a, const float* b, int32_t head_dim) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a == nullptr || b == nullptr || (x < y ? y - x : x - y) >= (uintptr_t)head_dim * sizeof(float);
+}
+
 pbb::NormArgs norm_args(const pbb_norm_t* norm, const pbb_rope_t* rope, double sign, int32_t n, int32_t hq,
                         int32_t hkv, const int32_t* positions) {
   pbb::NormArgs a{};
@@ -120,6 +126,7 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t* norm, const pbb_rope_t* 
   // (no tokens: the weights' gradients are zero, and have to be written)
   const bool sums = dq_weight != nullptr || (keys && dk_weight != nullptr);
   if (n_tokens == 0 && !sums) return PBB_OK;
+  if (keys && !sums_apart(dq_weight, dk_weight, head_dim)) return PBB_ERR_SHAPE;
   if (!aligned(dq_weight, 4) || (keys && !aligned(dk_weight, 4))) return PBB_ERR_ALIGN;
   if (n_tokens > 0) {
     if (!in_place_ok(q, q_stride, dq, dq_stride) || !in_place_ok(q_grad, q_grad_stride, dq, dq_stride) ||

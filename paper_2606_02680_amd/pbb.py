@@ -701,8 +701,8 @@ def pbb_norm_rotate_backward(rope, positions, q, q_grad, dq, k=None, k_grad=None
                              workspace=None, stream=None):
     """Gradients of :func:`pbb_norm_rotate` (whose inputs ``q`` and ``k`` are) for the gradients ``q_grad``
     and ``k_grad`` of its outputs: ``dq`` and ``dk``, and the weights' ``dq_weight`` and ``dk_weight``
-    (float32 [d], None: not wanted).  ``dq`` may be ``q_grad`` or ``q``.  Allocates the workspace when none
-    is given."""
+    (float32 [d], None: not wanted; two tensors, also for a weight that both share, whose gradient is their
+    sum).  ``dq`` may be ``q_grad`` or ``q``.  Allocates the workspace when none is given."""
     dev, dtype, code, hq, hkv, shape, at = _norm_call(rope, positions, q, k)
     if (k is None) != (k_grad is None) or (k is None) != (dk is None):
         raise ValueError("pbb_norm_rotate_backward: pass k, k_grad and dk, or none of them")
@@ -783,8 +783,8 @@ def _expect_coded(desc: PbbPagedDesc, pos, table, q_start, k_pages, v_pages, k_s
 
 
 def pbb_coded_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, k_scales, v_scales,
-                      q_start=None, rope=None, rope_pos=None, q=None, q_out=None, eps=None, q_weight=None,
-                      k_weight=None, stream=None):
+                     q_start=None, rope=None, rope_pos=None, q=None, q_out=None, eps=None, q_weight=None,
+                     k_weight=None, stream=None):
     """Append the new tokens of every sequence to an 8-bit cache (see ``include/pbb.h``): arguments as
     :func:`pbb_paged_append`; with ``eps``, keys and queries are normalised and weighted as
     :func:`pbb_norm_rotate` does before ``rope`` turns them."""
@@ -815,7 +815,7 @@ def pbb_coded_append(desc: PbbPagedDesc, pos, table, k, v, k_pages, v_pages, k_s
 
 
 def pbb_coded_read(desc: PbbPagedDesc, pos, table, k_pages, v_pages, k_scales, v_scales, k, v,
-                    q_start=None, stream=None):
+                   q_start=None, stream=None):
     """The values that the cache holds at the packed tokens' positions, into ``k`` and ``v``
     [tokens][Hkv][d] (bfloat16, exact; see ``include/pbb.h``)."""
     dev = _device_for("k", k, "[tokens][Hkv][d]")
@@ -832,7 +832,7 @@ def pbb_coded_read(desc: PbbPagedDesc, pos, table, k_pages, v_pages, k_scales, v
 
 
 def pbb_coded_attention(desc: PbbPagedDesc, pos, table, q, k_pages, v_pages, k_scales, v_scales, out,
-                         q_start=None, lse=None, workspace=None, stream=None):
+                        q_start=None, lse=None, workspace=None, stream=None):
     """:func:`pbb_paged_attention` over an 8-bit cache (see ``include/pbb.h``).  ``workspace``: of
     :func:`alloc_coded_workspace`, contiguous; allocated when none is given."""
     dev = _device_for("q", q, "[tokens][Hq][d]")

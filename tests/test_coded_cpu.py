@@ -99,6 +99,10 @@ def test_norm_backward_outputs():
     assert _backward(dq=A, dqs=1024) == SHAPE and _backward(dq=2 * A, dqs=1024) == SHAPE
     assert _backward(dk=5 * A, dks=256) == SHAPE
     assert _backward(dqw=A + 2) == ALIGN and _backward(dkw=A + 1) == ALIGN
+    # both kinds' sums in one array, or a part of one
+    for dqw, dkw in ((7 * A, 7 * A), (7 * A, 7 * A + 252), (7 * A + 128, 7 * A)):
+        assert _backward(dqw=dqw, dkw=dkw, ws=A, nbytes=1 << 20) == SHAPE
+        assert _backward(n=0, dqw=dqw, dkw=dkw) == SHAPE
     need = P.norm_workspace_bytes(4, 8, 2, 64, torch.bfloat16)
     assert need == 2 * 64 * 4                                   # one workgroup of each kind
     assert _backward(dqw=A) == WORKSPACE and _backward(dkw=A, ws=A, nbytes=need - 1) == WORKSPACE
