@@ -365,14 +365,20 @@ struct Wide {
   static constexpr int ALL = LDS > Narrow<D>::LDS ? LDS : Narrow<D>::LDS;
 };
 
-// read_chunks of 64 channels (those of the line that the addresses lie in).
-template <int D, int OFF>
-__device__ __forceinline__ void read_half_chunks(u32x2 (&dst)[8], const uint32_t (&ta)[4], uint32_t sb) {
+// The transposed operands of 32 of a tile's channels, 32 PART .. + 31, as read_chunks has them; wait_part: until
+// at most N LDS reads issued after them are on their way.
+template <int D, int OFF, int PART>
+__device__ __forceinline__ void read_part(u32x2 (&dst)[4], const uint32_t (&ta)[4], uint32_t sb) {
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    dst[2 * x] = tr_read<OFF>(ta[x] + sb);
-    dst[2 * x + 1] = tr_read<OFF + 32 * D>(ta[x] + sb);
+  for (int x = 0; x < 2; ++x) {
+    constexpr int AT = OFF + (PART >> 1) * kTileLine;
+    dst[2 * x] = tr_read<AT>(ta[2 * (PART & 1) + x] + sb);
+    dst[2 * x + 1] = tr_read<AT + 32 * D>(ta[2 * (PART & 1) + x] + sb);
   }
+}
+template <int N>
+__device__ __forceinline__ void wait_part(u32x2 (&v)[4]) {
+  asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]) : "i"(N));
 }
 
 // Table entry i >= 0, through the scalar cache, by a 32-bit byte offset (a width is at most 2^26; the 64-bit
@@ -678,30 +684,38 @@ void coded_kernel(CodedArgs a8) {
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) lsum[qc] += ps[qc];
     __builtin_amdgcn_s_setprio(kValuePriority);
-    // 64 channels' values at a time: 16 registers less than all at once, which the rows on their way need
+    // 32 channels' values at a time, the next 32's on their way (five chunks 1366 us; 64 at a time, none on
+    // their way, 1383; all at once, or the first ones' reads under the weights, spills into every step: 1429
+    // and 1774)
+    u32x2 vr[2][4];
+    read_part<D, L::TILE, 0>(vr[0], va, sb);
     auto values_of = [&](auto part) {
       constexpr int H = decltype(part)::value;
-      u32x2 vr[8];
-      read_half_chunks<D, L::TILE + H * kTileLine>(vr, va, sb);
-      wait_chunks<64>(vr);
-      if (masked && __builtin_amdgcn_ballot_w64(any_special(vr)) != 0) {
+      if constexpr (H + 1 < D / 32) read_part<D, L::TILE, H + 1>(vr[(H + 1) & 1], va, sb);
+      u32x2 (&v)[4] = vr[H & 1];
+      wait_part<H + 1 < D / 32 ? 4 : 0>(v);
+      if (masked && __builtin_amdgcn_ballot_w64(any_special(v)) != 0) {
         odd = true;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) vr[i][e] &= ~special_halves(vr[i][e]);
+          for (int e = 0; e < 2; ++e) v[i][e] &= ~special_halves(v[i][e]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bf16x8 vt = join_chunks(vr[2 * i], vr[2 * i + 1]);
+      for (int i = 0; i < 2; ++i) {
+        const bf16x8 vt = join_chunks(v[2 * i], v[2 * i + 1]);
 #pragma unroll
         for (int qc = 0; qc < QC; ++qc)
-          acc[qc][4 * H + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pB[qc], acc[qc][4 * H + i], 0, 0, 0);
+          acc[qc][2 * H + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pB[qc], acc[qc][2 * H + i], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
     values_of(std::integral_constant<int, 0>{});
-    if constexpr (D == 128) values_of(std::integral_constant<int, 1>{});
+    values_of(std::integral_constant<int, 1>{});
+    if constexpr (D == 128) {
+      values_of(std::integral_constant<int, 2>{});
+      values_of(std::integral_constant<int, 3>{});
+    }
     __builtin_amdgcn_s_setprio(kNoPriority);
   };
 
