@@ -478,8 +478,8 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t *norm, const pbb_rope_t *
  * (those exponents).  Of two tokens of a call that share a row, the codes and the byte may be of either.
  *
  * pbb_coded_append: arguments as pbb_paged_append; norm (optional) divides and weights keys and queries
- * as pbb_norm_rotate does, before rope turns them, all in fp32 and rounded once: to codes (keys), to
- * bfloat16 (q_out).  Values are quantised as they come.
+ * as pbb_norm_rotate does, before rope turns them, and rounds once: queries from fp32 to bfloat16 (q_out), bit
+ * for bit pbb_norm_rotate's, keys from fp64 to codes.  Values are quantised as they come.
  */
 pbb_status_t pbb_coded_append(const pbb_paged_desc_t *desc, int32_t n_tokens, const int32_t *pos,
                               const int32_t *q_start, const int32_t *table, const pbb_norm_t *norm,

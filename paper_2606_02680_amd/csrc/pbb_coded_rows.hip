@@ -1,14 +1,14 @@
 // Appending to an 8-bit paged cache, and reading it back, on gfx950 (MI355X).
 //
-// The append takes a chunk's new keys through the norm and the rotation (pbb_norm.hip has the formulas),
-// all in fp32, and rounds once, to e4m3 codes under the row's power of two (pbb_coded_device.h); values
-// are quantised as they come, queries go out as bf16 rows.  Reading back is exact: a code times a power
+// The append takes a chunk's new keys through the norm and the rotation (pbb_norm.hip has the formulas) in
+// fp64 and rounds once, to e4m3 codes under the row's power of two (pbb_coded_device.h); values are
+// quantised as they come, queries go out as bf16 rows, by way of fp32.  Reading back is exact: a code times a power
 // of two is a bf16 value.
 //
 // Bound: HBM (each row read once and written once), small calls by the launch.  Append: a lane takes 8
 // channels and their partners d/2 further on, as in the rotation, and writes 8 codes of each half.  9070
-// tokens of 32/8 heads, d 128, normed and turned: 40.2 us, 5.1 TB/s with its inputs in the last-level cache
-// (48.7 with the sines of a token worked out by each of its rows' lanes); 256 tokens: 5.5 us.
+// tokens of 32/8 heads, d 128, normed and turned: 43.0 us, 4.8 TB/s with its inputs in the last-level cache;
+// 256 tokens: 6.8 us.
 
 #include "pbb_norm_internal.h"
 #include "pbb_coded_device.h"
@@ -71,6 +71,68 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {   // over the PC (4 or
   if constexpr (PC >= 8) x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));
   return x;
 }
+template <int CTRL>
+__device__ __forceinline__ double add_dpp64(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, true);
+  return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int PC>
+__device__ __forceinline__ double row_sum64(double x) {   // row_sum in fp64, PC 4 or 8
+  x = add_dpp64<0x4E>(add_dpp64<0xB1>(x));
+  if constexpr (PC >= 8) x = add_dpp64<0x141>(x);
+  return x;
+}
+
+// To fp32: bits are cut off, and the last one is set where any of them was: what rounds the result once more, to
+// fewer bits, gives what rounding x itself would.
+__device__ __forceinline__ float to_odd(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t cut = (uint32_t)u & 0x1FFFFFFFu;   // (below fp32's 24 bits)
+  const float f = (float)__builtin_bit_cast(double, u ^ cut);
+  return __uint_as_float(__float_as_uint(f) | (cut < 1u ? cut : 1u));
+}
+
+// A key's piece through the norm and the rotation in fp64, so that its codes are those of the exact values
+// (in fp32 one value in 400 thousand falls over a border between codes): 9070 tokens of 32/8 heads take 43.0 us
+// so, 40.2 in fp32, 16000 of 12/2 heads, d 64, whose waves work on a token's queries, keys and values at once, 29
+// and 20.  (fp32 first, and this only for rows with a value near a border, one in a hundred: 44.3; 256 tokens 8.3
+// us, 6.8 so.)  Products with the weights are exact in fp32 (16 bits).
+template <int PC, int D>
+__device__ __forceinline__ void exact_key(const CodedAppendArgs& a, u32x4 wl, u32x4 wh, const double2* turns,
+                                          float (&y)[8], float (&z)[8]) {
+  typedef Piece<uint16_t> P;
+  double r = 1.0;
+  if (a.norm) {
+    double ss = 0.0;
+#pragma unroll
+    for (int e = 0; e < P::N; ++e) {
+      const double s = y[e], t = z[e];
+      ss = __builtin_fma(s, s, __builtin_fma(t, t, ss));
+    }
+    const double v = __builtin_fma(row_sum64<PC>(ss), 1.0 / D, (double)a.eps);
+    // 1 / sqrt(v) from fp32's by one of Newton's steps, v brought near 1 by a power of four
+    const int k = __builtin_amdgcn_frexp_exp(v) >> 1;
+    const double w = __builtin_ldexp(v, -2 * k);
+    r = (double)(1.0f / __builtin_sqrtf((float)w));
+    r = v < (double)INFINITY || v != v ? __builtin_ldexp(r * __builtin_fma(-0.5 * w * r, r, 1.5), -k) : 0.0;
+  }
+#pragma unroll
+  for (int e = 0; e < P::N; ++e) {
+    double s = y[e], t = z[e];
+    if (a.norm) s = y[e] * P::get(wl, e), t = z[e] * P::get(wh, e);
+    if (a.turn) {
+      const double2 u = turns[e];
+      const double x = __builtin_fma(s, u.x, -(t * u.y));
+      t = __builtin_fma(t, u.x, s * u.y);
+      s = x;
+    }
+    y[e] = to_odd(s * r), z[e] = to_odd(t * r);
+    __builtin_amdgcn_sched_barrier(0);   // (a pair at a time: registers)
+  }
+}
+
 // Grid: x (and z) = groups of tokens / waves per workgroup, y = runs of a token's query rows, key rows and
 // value rows (in this order).
 template <int D>
@@ -80,7 +142,7 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
   constexpr int ROWB = D * 2;
   constexpr int PC = ROWB / 32;
   constexpr int ROWS = 64 / PC;
-  __shared__ __align__(16) float2 turns[kRotThreads / 64][64];
+  __shared__ __align__(16) double2 turns[kRotThreads / 64][ROWS * D / 4];   // (a token has two rows or more)
   const int lane = threadIdx.x & 63;
   const int tpw = a.tokens_per_wave;
   const int64_t first = ((int64_t)token_group() * (kRotThreads / 64) +
@@ -112,13 +174,15 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
   };
   const Pair wq = weight(a.q_weight), wk = weight(a.k_weight);
   const Place at = place_of(a, tok, (int)first, last, lane);
-  if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
   float cs[N], sn[N];
-  if (a.turn) {   // (to fp32: the hardware's sines, good to 2^-20, move twice as many values over a code's border)
-    auto position = [&](int axis) { return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + tok] : at.t; };
-    if (tpw == 1) wave_turns<T, float, D>(a.rope, lane, pc, turns[threadIdx.x >> 6], position, cs, sn);
-    else piece_turns<T, float>(a.rope, pc, position, cs, sn);
-  }
+  double2* const wave = turns[threadIdx.x >> 6];
+  if (a.turn)
+    wave_turns<T, D>(a.rope, lane, pc, sub, tpw, wave, [&](int axis, int j) {
+      const int t = __shfl(at.t, j * rows * PC);   // (the first lane of token j)
+      return a.rope_pos != nullptr ? a.rope_pos[(size_t)axis * a.n + min((int)first + j, last)] : t;
+    }, cs, sn);
+  if (at.b < 0 || sub >= tpw || first + sub >= a.n) return;
+  const double2* const own = wave + sub * (D / 2) + pc * N;
   for (; r < r1; r += ROWS) {
     const bool query = r < hq, value = r >= hq + a.hkv;
     const u32x4 lo = next.lo, hi = next.hi;
@@ -126,26 +190,25 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
     float y[N], z[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = Piece<T>::get(lo, e), z[e] = Piece<T>::get(hi, e);
-    if (a.norm && !value) {
-      float ss = 0.0f;
-#pragma unroll
-      for (int e = 0; e < N; ++e) ss = __builtin_fmaf(y[e], y[e], __builtin_fmaf(z[e], z[e], ss));
-      const float rs = 1.0f / __builtin_sqrtf(__builtin_fmaf(row_sum<PC>(ss), 1.0f / D, a.eps));
-      const u32x4 wl = query ? wq.lo : wk.lo, wh = query ? wq.hi : wk.hi;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        y[e] = y[e] * rs * Piece<T>::get(wl, e);
-        z[e] = z[e] * rs * Piece<T>::get(wh, e);
-      }
-    }
-    if (a.turn && !value) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float s = y[e], t = z[e];
-        rope_turn(s, t, cs[e], sn[e], y[e], z[e]);
-      }
-    }
     if (query) {
+      if (a.norm) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) ss = __builtin_fmaf(y[e], y[e], __builtin_fmaf(z[e], z[e], ss));
+        const float rs = 1.0f / __builtin_sqrtf(__builtin_fmaf(row_sum<PC>(ss), 1.0f / D, a.eps));
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          y[e] = y[e] * rs * Piece<T>::get(wq.lo, e);
+          z[e] = z[e] * rs * Piece<T>::get(wq.hi, e);
+        }
+      }
+      if (a.turn) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float s = y[e], t = z[e];
+          rope_turn(s, t, cs[e], sn[e], y[e], z[e]);
+        }
+      }
       unsigned char* w = (unsigned char*)a.q_out + ((size_t)tok * hq + r) * ROWB + pc * 16;
       const u32x4 none = {0u, 0u, 0u, 0u};
       *(u32x4*)w = at.skip ? none : Piece<T>::put(y);
@@ -153,6 +216,7 @@ __global__ __launch_bounds__(kRotThreads) void coded_append_kernel(CodedAppendAr
       continue;
     }
     if (at.row < 0) break;   // (the rows after it are keys and values too)
+    if (!value && (a.norm || a.turn)) exact_key<PC, D>(a, wk.lo, wk.hi, own, y, z);
     uint32_t most = 0;
 #pragma unroll
     for (int e = 0; e < N; ++e) {

@@ -53,16 +53,6 @@ __device__ __forceinline__ void store16(u32x4 v, unsigned char* p) {
   else *(u32x4*)p = v;
 }
 
-// The sines and cosines of this lane's piece of a row of token tok, to fp32 in bf16 too, as in the 8-bit
-// append (pbb_coded_rows.hip), whose queries are these bit for bit.
-template <typename T, int D>
-__device__ __forceinline__ void token_turns(const NormArgs& a, const NormPart& p, int64_t tok, int lane, int pc,
-                                            float2* turns, float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
-  auto position = [&](int axis) { return a.positions[(size_t)axis * a.n + tok]; };
-  if (p.tokens_per_wave == 1) wave_turns<T, float, D>(a.rope, lane, pc, turns, position, cs, sn);
-  else piece_turns<T, float>(a.rope, pc, position, cs, sn);
-}
-
 // Workgroups 0 .. part[0].blocks - 1 take queries, the others keys.  A unit of work is a run of heads of
 // the tokens of a workgroup's waves; where a kind has fewer heads than a wave takes rows, a wave takes
 // several tokens.  Queries and keys in one launch: of small calls the launch is all (one token of 12/2 heads:
@@ -74,22 +64,26 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_kernel(NormArgs a) {
   constexpr int ROWB = D * (int)sizeof(T);
   constexpr int PC = ROWB / 32;
   constexpr int ROWS = 64 / PC;
-  __shared__ __align__(16) float2 turns[kNormThreads / 64][64];
+  __shared__ __align__(16) float2 turns[kNormThreads / 64][ROWS * D / 2];
   const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const bool keys = (int)blockIdx.x >= a.part[0].blocks;
   const NormPart& p = a.part[keys ? 1 : 0];
   const int block = (int)blockIdx.x - (keys ? a.part[0].blocks : 0);
   const int row = lane / PC, pc = lane % PC;
   const int sub = p.tokens_per_wave > 1 ? p.by_heads.div(row) : 0;
-  if (sub >= p.tokens_per_wave) return;
   const Weights<T> w(p.weight, pc, ROWB / 2);
   for (int u = block; u < p.units; u += p.blocks) {
     const int group = p.by_runs.div(u);
     const int first = (u - group * (int)p.by_runs.d) * p.run;
-    const int64_t tok = ((int64_t)group * (kNormThreads / 64) + (threadIdx.x >> 6)) * p.tokens_per_wave + sub;
-    if (tok >= a.n) continue;
+    const int64_t tok0 = ((int64_t)group * (kNormThreads / 64) + wave) * p.tokens_per_wave, tok = tok0 + sub;
+    if (tok0 >= a.n) continue;
     float cs[N], sn[N];
-    if (a.turn) token_turns<T, D>(a, p, tok, lane, pc, turns[threadIdx.x >> 6], cs, sn);
+    if (a.turn)   // (rounded once to fp32, in bf16 too, as in the 8-bit append, whose queries are these bit for bit)
+      wave_turns<T, D>(a.rope, lane, pc, sub, p.tokens_per_wave, turns[wave], [&](int axis, int j) {
+        return a.positions[(size_t)axis * a.n + min(tok0 + j, (int64_t)a.n - 1)];
+      }, cs, sn);
+    if (sub >= p.tokens_per_wave || tok >= a.n) continue;
     const unsigned char* x = (const unsigned char*)p.x + tok * p.x_stride + pc * 16;
     unsigned char* o = (unsigned char*)p.out + tok * p.out_stride + pc * 16;
     const int h1 = min(p.heads, first + p.run);
@@ -129,9 +123,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
   constexpr int ROWS = 64 / PC;
   constexpr int NW = kNormThreads / 64;
   __shared__ float sums[NW][D];
-  __shared__ __align__(16) float2 turns[NW][64];
+  __shared__ __align__(16) float2 turns[NW][ROWS * D / 2];
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const bool keys = (int)blockIdx.x >= a.part[0].blocks;
   const NormPart& p = a.part[keys ? 1 : 0];
   const int block = (int)blockIdx.x - (keys ? a.part[0].blocks : 0);
@@ -143,8 +137,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
   for (int e = 0; e < N; ++e) dlo[e] = dhi[e] = 0.0f;
   struct Pair { u32x4 xl, xh, gl, gh; };   // a row's piece and its gradient's
   for (int u = block; u < p.units; u += p.blocks) {
-    const int64_t tok = ((int64_t)u * NW + wave) * p.tokens_per_wave + sub;
-    if (tok >= a.n || sub >= p.tokens_per_wave) continue;
+    const int64_t tok0 = ((int64_t)u * NW + wave) * p.tokens_per_wave;
+    if (tok0 >= a.n) continue;
+    const int64_t tok = min(tok0 + min(sub, p.tokens_per_wave - 1), (int64_t)a.n - 1);
     const unsigned char* x = (const unsigned char*)p.x + tok * p.x_stride + pc * 16;
     const unsigned char* gr = (const unsigned char*)p.grad + tok * p.grad_stride + pc * 16;
     unsigned char* o = (unsigned char*)p.out + tok * p.out_stride + pc * 16;
@@ -157,7 +152,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_backward_kernel(Norm
     int h = row - sub * p.heads;
     Pair r0 = load(min(h, p.heads - 1));
     float cs[N], sn[N];
-    if (a.turn) token_turns<T, D>(a, p, tok, lane, pc, turns[threadIdx.x >> 6], cs, sn);
+    if (a.turn)
+      wave_turns<T, D>(a.rope, lane, pc, sub, p.tokens_per_wave, turns[wave], [&](int axis, int j) {
+        return a.positions[(size_t)axis * a.n + min(tok0 + j, (int64_t)a.n - 1)];
+      }, cs, sn);
+    if (sub >= p.tokens_per_wave || tok0 + sub >= a.n) continue;
     for (; h < p.heads; h += ROWS) {
       const size_t at = (size_t)h * ROWB;
       const Pair v = r0;

@@ -60,36 +60,67 @@ __device__ __forceinline__ void cos_sin(double turns, float& cs, float& sn) {
   }
 }
 
+// A constant of an fp64 sum, in scalar registers where it is used (else the compiler keeps all of a sum's in
+// vector registers throughout the kernel: 98 instead of 84 in the norms').
+__device__ __forceinline__ double scalar_constant(double x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+// cos and sin of `turns` whole turns to some 2^-36: of what is left of the nearest quarter turn, an eighth of a
+// turn either way, by their Taylor sums.
+__device__ __forceinline__ void cos_sin64(double turns, double& cs, double& sn) {
+  const double f = turns - __builtin_rint(turns), quarter = __builtin_rint(4.0 * f);
+  const double x = (f - 0.25 * quarter) * scalar_constant(6.283185307179586477), z = x * x;
+  auto next = [&](double sum, double k) { return __builtin_fma(sum, z, scalar_constant(k)); };
+  double s = __builtin_fma(z, scalar_constant(-1.0 / 39916800.0), scalar_constant(1.0 / 362880.0));
+  s = next(next(next(s, -1.0 / 5040.0), 1.0 / 120.0), -1.0 / 6.0);
+  s = __builtin_fma(s * z, x, x);
+  double c = __builtin_fma(z, scalar_constant(1.0 / 479001600.0), scalar_constant(-1.0 / 3628800.0));
+  c = next(next(next(c, 1.0 / 40320.0), -1.0 / 720.0), 1.0 / 24.0);
+  c = __builtin_fma(__builtin_fma(c, z, -0.5), z, 1.0);
+  const int q = (int)quarter & 3;
+  const double a = q & 1 ? s : c, b = q & 1 ? c : s;
+  cs = q == 1 || q == 2 ? -a : a;
+  sn = q >= 2 ? -b : b;
+}
+
 // The sines and cosines of piece pc of a row (pairs pc N .. + N - 1) at a token's positions;
-// position(axis) reads them.  A: those of cos_sin<A>.
-template <typename T, typename A = T, typename F>
+// position(axis) reads them.
+template <typename T, typename F>
 __device__ __forceinline__ void piece_turns(const RopeArgs& r, int pc, F&& position,
                                             float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
   constexpr int N = Piece<T>::N;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     const int c = pc * N + e;
-    cos_sin<A>((double)position(r.axis[c]) * r.turns[c], cs[e], sn[e]);
+    cos_sin<T>((double)position(r.axis[c]) * r.turns[c], cs[e], sn[e]);
   }
 }
 
-// The same for a wave whose lanes all work on one token: each lane works out one pair and takes its piece's
-// from the others through LDS (`turns`: 64 float2 of the wave's own).  piece_turns does the work of a
-// token once per row of the wave, which its fp64 steps and, in fp32, its sines dominate (9070 tokens
-// appended: 48.7 us so, 40.0 shared; 4 x 16384 tokens normalised 245 and 231).
-template <typename T, typename A, int D, typename F>
-__device__ __forceinline__ void wave_turns(const RopeArgs& r, int lane, int pc, float2* turns, F&& position,
-                                           float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
+// The same, rounded once from cos_sin64, for a wave that works on `tokens` tokens, this lane on the one with
+// index `sub`: the lanes work out a pair each and take their pieces' from one another through LDS (`turns`:
+// tokens * D / 2 of the wave's own, float2 or double2, which stay there).  position(axis, j): of token j.  All
+// lanes take part.  (With piece_turns' sums, whose fp64 steps each row of the wave does again, 9070 tokens
+// took 48.7 us to append, 40.0 shared; 4 x 16384 tokens 245 and 231 to norm.)
+template <typename T, int D, typename V, typename F>
+__device__ __forceinline__ void wave_turns(const RopeArgs& r, int lane, int pc, int sub, int tokens, V* turns,
+                                           F&& position, float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
   constexpr int N = Piece<T>::N;
-  const int c = lane & (D / 2 - 1);
-  float2 t;
-  cos_sin<A>((double)position(r.axis[c]) * r.turns[c], t.x, t.y);
-  turns[lane] = t;
+#pragma unroll 1
+  for (int i = lane; i < tokens * (D / 2); i += 64) {
+    const int j = i / (D / 2), c = i % (D / 2);
+    double cd, sd;
+    cos_sin64((double)position(r.axis[c], j) * r.turns[c], cd, sd);
+    V t;
+    t.x = cd, t.y = sd;
+    turns[i] = t;
+  }
   __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses keep their order)
+  const V* const own = turns + min(sub, tokens - 1) * (D / 2) + pc * N;
 #pragma unroll
-  for (int e = 0; e < N; e += 2) {
-    const f32x4 two = *(const f32x4*)(turns + pc * N + e);
-    cs[e] = two[0], sn[e] = two[1], cs[e + 1] = two[2], sn[e + 1] = two[3];
+  for (int e = 0; e < N; ++e) {
+    const V u = own[e];
+    cs[e] = (float)u.x, sn[e] = (float)u.y;
   }
   __builtin_amdgcn_wave_barrier();
 }

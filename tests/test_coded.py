@@ -160,6 +160,42 @@ def test_append_and_read(cuda, norm, d, hq, hkv, page, axes, lens, uniform):
         assert torch.equal(got.cpu().double(), want)
 
 
+@pytest.mark.parametrize("d,hkv,hq,axes,norm", [(64, 2, 12, 1, True), (128, 8, 0, 3, True), (128, 4, 16, 1, False),
+                                                (64, 1, 0, 0, True), (64, 4, 8, 2, True)])
+def test_keys_have_the_codes_of_exact_values(cuda, d, hkv, hq, axes, norm):
+    """Norm and rotation of keys in 64 bits: their codes and scale bytes are those of the exact result, but
+    for values so near a border between codes that 2^-33 of their pair (the sines are good to 2^-36, the
+    rates and the angle's reduction to 2^-36 of a turn at these positions) decides."""
+    n = 4000
+    c = Coded([(5, n)], hq or hkv, hkv, d, 64, seed=d + hkv + axes)
+    g = torch.Generator().manual_seed(3)
+    c.k = c.k * torch.exp(3 * torch.randn(c.n, hkv, 1, generator=g)).to(BF)
+    weight = (1 + 0.3 * torch.randn(d, generator=g)).to(BF) if norm else None
+    axis = _axis(d, axes) if axes else None
+    rope = P.make_rope(d, BASE, axis if axes > 1 else None) if axes else None
+    positions = torch.randint(0, 20000, (max(axes, 1), c.n), generator=g).to(torch.int32)
+    x = c.on(cuda)
+    more = dict(eps=EPS, k_weight=weight.to(cuda)) if norm else {}
+    if hq:
+        more |= dict(q=x["q"], q_out=torch.empty_like(x["q"]))
+    P.pbb_coded_append(c.desc(), x["pos"], x["table"], x["k"], x["v"], *_pool(x), q_start=x["q_start"], rope=rope,
+                       rope_pos=positions.to(cuda) if axes else None, **more)
+    at = 5 + torch.arange(n)
+    page, slot = c.table[0, at // 64].long(), at % 64
+    codes, scales = (x[t].view(U8).cpu()[page, :, slot] for t in ("k_pages", "k_scales"))
+    k = c.k[:n] if c.n == n else c.k
+    y = C.norm_rotate(k, weight, EPS) if norm else k.double()
+    want = R.rotate(y, positions, axis, BASE) if axes else y
+    d2 = 2.0 ** -33 * (y[..., :d // 2].abs() + y[..., d // 2:].abs())
+    size = torch.cat((d2, d2), dim=-1)
+    low, high = (C.encode(want + sign * size * want.sign()) for sign in (-1, 1))
+    sure = low[0].view(U8) == high[0].view(U8)
+    even = low[1] == high[1]
+    assert float(sure.double().mean()) > 0.999999 and bool(even.all())
+    assert torch.equal(scales, low[1])
+    assert torch.equal(codes[sure], low[0].view(U8)[sure])
+
+
 def test_extreme_rows(cuda):
     """Zeros, the smallest and the largest magnitudes, infinities and NaN, borders of the power of two:
     the reference's codes; and every code under every byte that an append may write, read back."""
