@@ -95,10 +95,11 @@ __device__ __forceinline__ float to_odd(double x) {
 }
 
 // A key's piece through the norm and the rotation in fp64, so that its codes are those of the exact values
-// (in fp32 one value in 400 thousand falls over a border between codes): 9070 tokens of 32/8 heads take 43.0 us
-// so, 40.2 in fp32, 16000 of 12/2 heads, d 64, whose waves work on a token's queries, keys and values at once, 29
-// and 20.  (fp32 first, and this only for rows with a value near a border, one in a hundred: 44.3; 256 tokens 8.3
-// us, 6.8 so.)  Products with the weights are exact in fp32 (16 bits).
+// (in fp32 one value in 400 thousand falls over a border between codes).  Appended and read back, 9070 tokens of
+// 32/8 heads, d 128, take 57.7 us so, 55.5 with keys in fp32; 16000 of 12/2 heads, d 64, whose waves work on a
+// token's queries, keys and values at once, 35.2 and 26.7; 256 of 32/8 8.7 and 7.7.  (fp32 first, and this for
+// rows with a value near a border, of which there is one in a hundred: 59.0, 34.7, 10.3.)  Products with the
+// weights are exact in fp32 (16 bits).
 template <int PC, int D>
 __device__ __forceinline__ void exact_key(const CodedAppendArgs& a, u32x4 wl, u32x4 wh, const double2* turns,
                                           float (&y)[8], float (&z)[8]) {

@@ -107,8 +107,9 @@ __device__ __forceinline__ void wave_turns(const RopeArgs& r, int lane, int pc, 
                                            F&& position, float (&cs)[Piece<T>::N], float (&sn)[Piece<T>::N]) {
   constexpr int N = Piece<T>::N;
 #pragma unroll 1
-  for (int i = lane; i < tokens * (D / 2); i += 64) {
-    const int j = i / (D / 2), c = i % (D / 2);
+  for (int first = 0; first < tokens * (D / 2); first += 64) {
+    // (lanes past the last pair do it again: position() may ask other lanes, which have to be there)
+    const int i = min(first + lane, tokens * (D / 2) - 1), j = i / (D / 2), c = i % (D / 2);
     double cd, sd;
     cos_sin64((double)position(r.axis[c], j) * r.turns[c], cd, sd);
     V t;

@@ -161,7 +161,8 @@ def test_append_and_read(cuda, norm, d, hq, hkv, page, axes, lens, uniform):
 
 
 @pytest.mark.parametrize("d,hkv,hq,axes,norm", [(64, 2, 12, 1, True), (128, 8, 0, 3, True), (128, 4, 16, 1, False),
-                                                (64, 1, 0, 0, True), (64, 4, 8, 2, True)])
+                                                (64, 1, 0, 0, True), (64, 4, 8, 2, True), (64, 1, 3, 1, True),
+                                                (64, 1, 1, 1, False), (128, 1, 1, 1, True), (64, 1, 5, 2, True)])
 def test_keys_have_the_codes_of_exact_values(cuda, d, hkv, hq, axes, norm):
     """Norm and rotation of keys in 64 bits: their codes and scale bytes are those of the exact result, but
     for values so near a border between codes that 2^-33 of their pair (the sines are good to 2^-36, the
@@ -174,12 +175,14 @@ def test_keys_have_the_codes_of_exact_values(cuda, d, hkv, hq, axes, norm):
     axis = _axis(d, axes) if axes else None
     rope = P.make_rope(d, BASE, axis if axes > 1 else None) if axes else None
     positions = torch.randint(0, 20000, (max(axes, 1), c.n), generator=g).to(torch.int32)
+    if axes == 1 and d == 64:   # the cache positions, from the 5 on that are cached
+        positions = (5 + torch.arange(c.n)).to(torch.int32)[None]
     x = c.on(cuda)
     more = dict(eps=EPS, k_weight=weight.to(cuda)) if norm else {}
     if hq:
         more |= dict(q=x["q"], q_out=torch.empty_like(x["q"]))
     P.pbb_coded_append(c.desc(), x["pos"], x["table"], x["k"], x["v"], *_pool(x), q_start=x["q_start"], rope=rope,
-                       rope_pos=positions.to(cuda) if axes else None, **more)
+                       rope_pos=positions.to(cuda) if axes > 1 or (axes == 1 and d == 128) else None, **more)
     at = 5 + torch.arange(n)
     page, slot = c.table[0, at // 64].long(), at % 64
     codes, scales = (x[t].view(U8).cpu()[page, :, slot] for t in ("k_pages", "k_scales"))
