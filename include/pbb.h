@@ -408,7 +408,8 @@ pbb_status_t pbb_paged_attention(const pbb_paged_desc_t *desc, int32_t n_tokens,
  * Norms of queries and keys for each head, with the rotation in the same pass: models that divide every
  * query and key row by its root mean square before they turn it.
  *   y = R(p) (x r w),  r = 1 / sqrt(mean_c x_c^2 + eps),  R(p) the rotation of pbb_rotate
- * in fp32 (a row's squares are summed in fp32: magnitudes up to about 1e18), rounded once.  eps > 0 and
+ * in fp32 (a row's squares are summed in fp32: magnitudes up to about 1e18), rounded once.  Angles are those of
+ * the exact product of position and rate, reduced to a turn, sines and cosines rounded once to fp32.  eps > 0 and
  * finite (PBB_ERR_SHAPE otherwise).  q_weight, k_weight: [head_dim] of the rows' type, device memory, 16-byte
  * aligned, NULL for ones.  The struct is plain data, read on the host at each call.
  */

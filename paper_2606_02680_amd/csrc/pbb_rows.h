@@ -61,15 +61,19 @@ __device__ __forceinline__ void cos_sin(double turns, float& cs, float& sn) {
 }
 
 // A constant of an fp64 sum, in scalar registers where it is used (else the compiler keeps all of a sum's in
-// vector registers throughout the kernel: 98 instead of 84 in the norms').
+// vector registers throughout the kernel).
 __device__ __forceinline__ double scalar_constant(double x) {
   asm volatile("" : "+s"(x));
   return x;
 }
-// cos and sin of `turns` whole turns to some 2^-36: of what is left of the nearest quarter turn, an eighth of a
-// turn either way, by their Taylor sums.
-__device__ __forceinline__ void cos_sin64(double turns, double& cs, double& sn) {
-  const double f = turns - __builtin_rint(turns), quarter = __builtin_rint(4.0 * f);
+// cos and sin of position * rate whole turns to some 2^-36: of what is left of the nearest quarter turn, an eighth
+// of a turn either way, by their Taylor sums.  The whole turns come off the exact product (31 bits times 53: a
+// rounded one would be off by half a turn and more at far positions and rates above 2^21), and twice, since
+// those of a product above 2^53 leave what its rounding took.
+__device__ __forceinline__ void cos_sin64(double position, double rate, double& cs, double& sn) {
+  const double part = __builtin_fma(position, rate, -__builtin_rint(position * rate));
+  const double f = part - __builtin_rint(part);
+  const double quarter = __builtin_rint(4.0 * f);
   const double x = (f - 0.25 * quarter) * scalar_constant(6.283185307179586477), z = x * x;
   auto next = [&](double sum, double k) { return __builtin_fma(sum, z, scalar_constant(k)); };
   double s = __builtin_fma(z, scalar_constant(-1.0 / 39916800.0), scalar_constant(1.0 / 362880.0));
@@ -111,7 +115,7 @@ __device__ __forceinline__ void wave_turns(const RopeArgs& r, int lane, int pc, 
     // (lanes past the last pair do it again: position() may ask other lanes, which have to be there)
     const int i = min(first + lane, tokens * (D / 2) - 1), j = i / (D / 2), c = i % (D / 2);
     double cd, sd;
-    cos_sin64((double)position(r.axis[c], j) * r.turns[c], cd, sd);
+    cos_sin64((double)position(r.axis[c], j), r.turns[c], cd, sd);
     V t;
     t.x = cd, t.y = sd;
     turns[i] = t;
