@@ -442,8 +442,8 @@ pbb_status_t pbb_norm_rotate(const pbb_norm_t *norm, const pbb_rope_t *rope, int
  *   q_grad, dq, k_grad, dk   rows as q and k, with strides of their own; dq may be q_grad or q, dk k_grad
  *              or k (same stride)
  *   dq_weight, dk_weight     optional float32 [head_dim], 4-byte aligned, overwritten (zeros for
- *              n_tokens == 0), two arrays (PBB_ERR_SHAPE where they overlap): a weight that queries and
- *              keys share has the sum of both for its gradient
+ *              n_tokens == 0, dk_weight for n_kv_heads == 0 too), two arrays (PBB_ERR_SHAPE where they
+ *              overlap): a weight that queries and keys share has the sum of both for its gradient
  * Deterministic.  workspace: pbb_norm_workspace_bytes bytes, 16-byte aligned, contents irrelevant; needed
  * with a weight's gradient only (PBB_ERR_WORKSPACE if NULL or smaller); calls that may run concurrently need
  * workspaces of their own.  The size depends on the arguments of its query alone and is at most

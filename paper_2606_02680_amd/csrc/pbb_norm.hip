@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kSumThreads) void norm_weight_sum_kernel(NormArgs a
   __shared__ f32x4 sums[kSumThreads / 64];
   const int kind = (int)blockIdx.x / (D / 4);
   const NormPart& p = a.part[kind];
-  if (p.dweight == nullptr || p.blocks == 1) return;   // (0 of a call of no tokens: zeros)
+  if (p.dweight == nullptr || p.blocks == 1) return;   // (0 of a call of no tokens or no heads: zeros)
   const int channel = ((int)blockIdx.x % (D / 4)) * 4;
   const float* parts = a.partials + (size_t)(kind ? a.part[0].blocks : 0) * D + channel;
   f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -273,9 +273,9 @@ hipError_t backward_t(const NormArgs& a0, hipStream_t stream) {
   NormArgs a = a0;
   bool more = false;
   for (NormPart& p : a.part) {
-    if (p.heads == 0) {
+    if (p.heads == 0) {   // (no rows: its weight's gradient is zeros)
       p.units = p.blocks = 0;
-      p.dweight = nullptr;
+      more |= p.dweight != nullptr;
       continue;
     }
     p.tokens_per_wave = norm_tokens_per_wave(p.heads, ROWS);

@@ -123,11 +123,11 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t* norm, const pbb_rope_t* 
   if (keys)
     for (int64_t s : {k_stride, k_grad_stride, dk_stride})
       if (!stride_ok(s, n_kv_heads, head_dim, u)) return PBB_ERR_SHAPE;
-  // (no tokens: the weights' gradients are zero, and have to be written)
-  const bool sums = dq_weight != nullptr || (keys && dk_weight != nullptr);
+  // (no tokens, or no heads of a kind: the weight's gradient is zero, and has to be written)
+  const bool sums = dq_weight != nullptr || dk_weight != nullptr;
   if (n_tokens == 0 && !sums) return PBB_OK;
-  if (keys && !sums_apart(dq_weight, dk_weight, head_dim)) return PBB_ERR_SHAPE;
-  if (!aligned(dq_weight, 4) || (keys && !aligned(dk_weight, 4))) return PBB_ERR_ALIGN;
+  if (!sums_apart(dq_weight, dk_weight, head_dim)) return PBB_ERR_SHAPE;
+  if (!aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return PBB_ERR_ALIGN;
   if (n_tokens > 0) {
     if (!in_place_ok(q, q_stride, dq, dq_stride) || !in_place_ok(q_grad, q_grad_stride, dq, dq_stride) ||
         (keys && (!in_place_ok(k, k_stride, dk, dk_stride) ||
@@ -140,7 +140,7 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t* norm, const pbb_rope_t* 
         (keys && (!aligned(k, 16) || !aligned(k_grad, 16) || !aligned(dk, 16) ||
                   !aligned(norm->k_weight, 16))))
       return PBB_ERR_ALIGN;
-    if (sums) {
+    if (dq_weight != nullptr || (keys && dk_weight != nullptr)) {
       const size_t need = backward_bytes(head_dim, n_tokens, n_q_heads, n_kv_heads, dtype);
       if (workspace == nullptr || workspace_bytes < need) return PBB_ERR_WORKSPACE;
       if (!aligned(workspace, 16)) return PBB_ERR_ALIGN;
@@ -154,7 +154,7 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t* norm, const pbb_rope_t* 
   a.part[1].x = k, a.part[1].x_stride = k_stride * u;
   a.part[1].grad = k_grad, a.part[1].grad_stride = k_grad_stride * u;
   a.part[1].out = dk, a.part[1].out_stride = dk_stride * u;
-  a.part[1].dweight = keys ? dk_weight : nullptr;
+  a.part[1].dweight = dk_weight;
   a.partials = static_cast<float*>(workspace);
   const hipError_t e = pbb::launch_norm_rotate_backward(a, head_dim, dtype == PBB_DTYPE_F32,
                                                         reinterpret_cast<hipStream_t>(stream));
