@@ -475,7 +475,7 @@ pbb_status_t pbb_norm_rotate_backward(const pbb_norm_t *norm, const pbb_rope_t *
  * What an append stores of a row: the least power 2^e, -100 <= e <= 119, under which the row's largest finite
  * magnitude is at most 448 (the largest code), and the codes of the quotients, nearest, ties to even, finite
  * ones cut to 448 (rows above 2^119 * 448) -- so each value to half a step, 2^-4 of itself, or 2^-10 of 2^e
- * where that is more.  Infinities and NaN are stored as NaN.  Other writers may use any byte from 27 to 246
+ * where that is more.  Infinities (turned keys above the largest float among them) and NaN are stored as NaN.  Other writers may use any byte from 27 to 246
  * (those exponents).  Of two tokens of a call that share a row, the codes and the byte may be of either.
  *
  * pbb_coded_append: arguments as pbb_paged_append; norm (optional) divides and weights keys and queries
@@ -505,6 +505,8 @@ pbb_status_t pbb_coded_read(const pbb_paged_desc_t *desc, int32_t n_tokens, cons
  * Attention of the packed tokens over the 8-bit cache: pbb_paged_attention of the values that codes and
  * scales stand for, with its supports, masks, empty supports and log-partitions.  Scores are products of the
  * unquantised queries with fp32 accumulation; the value products take weights as pbb_paged_attention does.
+ * Sums are taken before they are divided, of weights up to 2^8: values below 2^121 / n in size, n the keys of
+ * a support, cannot overflow them.
  * workspace: pbb_coded_workspace_bytes bytes, by the rules of pbb_paged_workspace_bytes (its first
  * PBB_PAGED_COUNTER_BYTES zero before the first call, and left zero).
  */

@@ -131,6 +131,23 @@ def test_dropped_pages(cuda):
         _check(c, cuda, block, window)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,hq,hkv,lens", [(64, 12, 2, [(63, 1), (0, 1), (17, 1), (40, 1)]),
+                                           (128, 8, 1, [(60, 2), (3, 1), (31, 1)]),
+                                           (128, 4, 1, [(20, 44), (0, 64)]), (64, 8, 2, [(47, 17), (9, 30)])])
+def test_values_of_every_power(cuda, d, hq, hkv, lens):
+    """Value rows of any power from the least to where a sum of the support's 64 keys cannot overflow: below
+    2^121 / 64, 448 times 2^106."""
+    c = _cache(lens, hq, hkv, d, 16, seed=d + hq, garbage=255)
+    g = torch.Generator().manual_seed(hq)
+    live = c.v_scales != 255
+    for powers in (torch.randint(27, 127 + 106, c.v_scales.shape, generator=g),
+                   torch.randint(27, 40, c.v_scales.shape, generator=g),
+                   torch.randint(127 + 96, 127 + 107, c.v_scales.shape, generator=g)):
+        c.v_scales = torch.where(live, powers.to(torch.uint8), c.v_scales)
+        _check(c, cuda)
+
+
 # ------------------------------------------------------------------------------------------
 # what the bounds tell apart (CPU)
 
