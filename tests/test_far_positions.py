@@ -12,8 +12,6 @@ from tests import coded_ref as C
 from tests.test_coded import BASE, BF, EPS, U8, Coded, _pool
 from tests.test_paged import _within
 
-F32 = torch.float32
-
 
 def turns_of(rate, position):
     """position * rate modulo 1, in [-2, 2]: halves of 16 bits of the position times halves of 27 of the rate,
